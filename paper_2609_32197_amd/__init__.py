@@ -31,6 +31,15 @@ Demand-directed KV routing (Section 5):
     sparsp_pack_for_consumers      a producer's packed blocks for every consumer
     sparsp_route_volume            dense / relay / direct block-hops (host)
 
+A growing sequence and its paged cache (paged.py, include/sparsp_cache.h):
+
+    sparsp_rope_frequencies        rotary frequencies, scaled for long contexts (host)
+    sparsp_rope                    rotary positions of Q and K, or back
+    sparsp_paged_append            new tokens into the cache, K and Q rotated on the way
+    sparsp_paged_attn              attention of the new tokens over the cache
+    sparsp_paged_weights           attention weight per cached token
+    sparsp_cache_evict             the cache cut to the tokens of most weight
+
 Short aliases without the prefix are provided as well.
 """
 
@@ -701,3 +710,8 @@ permute_blocks = sparsp_permute_blocks
 remote_demand = sparsp_remote_demand
 pack_for_consumers = sparsp_pack_for_consumers
 route_volume = sparsp_route_volume
+
+from . import paged as _paged  # noqa: E402  (it uses the helpers above)
+from .paged import *  # noqa: E402,F401,F403
+
+__all__ += _paged.__all__

@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "cache_launch.h"
 #include "sparsp_launch.h"
 
 namespace {
@@ -187,6 +188,15 @@ int attn_whole(const sparsp_geom* g, const void* Q, const int32_t* sel, int32_t 
 }
 
 }  // namespace
+
+namespace sparsp {
+
+int set_error(int code, const char* msg) {
+    snprintf(g_err, sizeof(g_err), "%s", msg);
+    return code;
+}
+
+}  // namespace sparsp
 
 extern "C" {
 

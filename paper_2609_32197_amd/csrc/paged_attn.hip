@@ -1,0 +1,388 @@
+// Attention of new tokens over the paged cache (Eq. 1 over a sequence's cached tokens).
+//
+// Rows. The query heads of one key head share its keys, so a row is (token, head of the
+// group), token-major: n new tokens of a group of G heads are n G rows, packed 16 to an
+// operand. A decoding step of G = 4 thus reads K and V once for four rows.
+//
+// paged_rows_kernel, for few rows: a workgroup takes 16 NC rows and a part of the
+// sequence's keys; its four waves walk the key tiles in turn (wave w the tiles w, w+4, ...),
+// each with a softmax of its own, loading the tile after next while they compute. The
+// waves' results are merged in LDS through their running maxima. What bounds it is
+// reading K and V, so every tile goes straight to operand registers (paged_tiles.h).
+//
+// Long caches are split: each part (a multiple of `step` keys) writes its normalised
+// output and lse, float32, to the workspace, and a merge kernel joins a row's parts in
+// their order. A sequence short enough for one part writes its output directly.
+#include <algorithm>
+
+#include "paged_tiles.h"
+
+namespace sparsp {
+namespace {
+
+constexpr int kCus = 256;
+
+// The launch's view of the work: `tiles` workgroups stride over a sequence's row tiles,
+// `parts` over its keys.
+struct Plan {
+    int tiles, parts, step;
+    float* part_o;    // [q_heads, tokens, parts, d]
+    float* part_lse;  // [q_heads, tokens, parts]
+};
+
+// Keys of a part of a sequence of kv cached tokens: a multiple of step, so many that
+// `parts` of them cover kv.
+__device__ __forceinline__ int part_keys(const Plan& p, int kv) {
+    const int64_t all = (int64_t(kv) + p.parts - 1) / p.parts;
+    const int64_t k = (all + p.step - 1) / p.step * p.step;
+    return int(k < p.step ? p.step : k);
+}
+
+__device__ __forceinline__ void store4(void* O, int64_t at, bool bf16, const float (&x)[4]) {
+    if (bf16) {
+        uint2 w;
+        w.x = f32_to_bf16_bits(x[0]) | (f32_to_bf16_bits(x[1]) << 16);
+        w.y = f32_to_bf16_bits(x[2]) | (f32_to_bf16_bits(x[3]) << 16);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(O) + at) = w;
+    } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(O) + at) =
+            make_float4(x[0], x[1], x[2], x[3]);
+    }
+}
+
+template <typename T, int D, int NC>
+__global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, const Plan plan) {
+    using M = TileMath<T, D>;
+    constexpr int KEYS = M::KEYS, DV = M::DV, PITCH = D + 4;
+    __shared__ float merge_o[4][16][PITCH];
+    __shared__ float merge_m[4][16], merge_l[4][16];
+    const sparsp_cache& c = a.cache;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    // The row tiles of one part of the keys run on one XCD, one after another, so that all
+    // but the first find the keys in its L2.
+    const int units = c.B * c.H * plan.parts;
+    const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
+    const int unit = k / plan.tiles * 8 + xcd;
+    if (unit >= units) return;
+    const int part = unit % plan.parts, bh = unit / plan.parts;
+    const int b = bh / c.H, hk = bh % c.H;
+    const int G = a.q_heads / c.H;
+    const Seq s = sequence(c, a.tokens, b);
+    const int rows = s.n * G;
+    const int keys = part_keys(plan, s.kv);
+    const bool whole = s.kv <= keys;
+    if (part > 0 && part * int64_t(keys) >= s.kv) return;
+    const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
+    const float c2 = a.scale * kLog2e;
+
+    for (int tile = k % plan.tiles; tile * int64_t(16 * NC) < rows; tile += plan.tiles) {
+        typename M::QTile q[NC];
+        int limit[NC], lowest = 1 << 30;  // keys before limit are seen
+        int end = 0;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const int r = (tile * NC + n) * 16 + col;
+            const bool live = r < rows;
+            const int i = live ? r / G : 0, h = hk * G + (live ? r % G : 0);
+            limit[n] = a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+            if (!live) limit[n] = 1 << 30;
+            lowest = min(lowest, limit[n]);
+            M::load_row(q[n], a.Q, int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token, live,
+                        c.d, lane);
+        }
+        {
+            const int last = min(rows, (tile + 1) * 16 * NC) - 1;
+            end = a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv;
+            end = min(end, part_end);
+        }
+
+        floatx4 acc[NC][DV];
+        float m[NC], l[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DV; ++d) acc[n][d] = floatx4{};
+        }
+
+        struct Stage {
+            typename M::KTile k;
+            typename M::VTile v;
+            int kp, vp;
+        };
+        auto load = [&](Stage& st, int t0, int kp, int vp) {
+            M::load_k(c, st.k, kp, hk, t0, lane);
+            M::load_v(c, st.v, vp, hk, t0, lane);
+            st.kp = kp;
+            st.vp = vp;
+        };
+        auto compute = [&](Stage& st, int t0) {
+            const bool masked =
+                __ballot(t0 + KEYS > lowest || t0 + KEYS > end || st.kp < 0 || st.vp < 0) != 0;
+            if (masked) {
+                // What lies behind the sequence may be anything, NaN included: rows of V there
+                // are zeroed, not multiplied by a probability of zero.
+                const int live = st.vp < 0 ? 0 : part_end - (t0 + M::v_group(lane));
+                M::clear_v(st.v, live);
+            }
+            typename M::P pr[NC];
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                floatx4 sc[M::U];
+                M::scores(st.k, q[n], sc);
+                float p[M::PER];
+#pragma unroll
+                for (int v = 0; v < M::PER; ++v) p[v] = sc[v / 4][v % 4];
+                if (masked) {
+                    const int lim = st.vp < 0 ? 0 : min(limit[n], part_end);
+#pragma unroll
+                    for (int v = 0; v < M::PER; ++v)
+                        p[v] = t0 + M::key_of(g, v) < lim ? p[v] : -INFINITY;
+                }
+                float mx = p[0];
+#pragma unroll
+                for (int v = 1; v < M::PER; ++v) mx = fmaxf(mx, p[v]);
+                mx = row_max(mx);
+                if (__ballot(mx > m[n]) != 0) {
+                    const float top = fmaxf(m[n], mx);
+                    const float alpha =
+                        top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * c2);
+                    m[n] = top;
+                    l[n] *= alpha;
+#pragma unroll
+                    for (int d = 0; d < DV; ++d) acc[n][d] *= alpha;
+                }
+                const float base = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+                for (int v = 0; v < M::PER; ++v) {
+                    p[v] = __builtin_amdgcn_exp2f((p[v] - base) * c2);
+                    l[n] += p[v];
+                }
+                pr[n] = M::pack(p);
+            }
+            M::template output<NC>(st.v, pr, acc);
+        };
+
+        // Two tiles in flight: one is computed while the next is loaded, and the page
+        // numbers of the one after that are on their way. (With 32 rows the registers hold
+        // one tile; the CU's other waves cover its loads.)
+        constexpr int JUMP = 4 * KEYS;
+        int t0 = lo + wave * KEYS;
+        if (t0 < end) {
+            Stage A;
+            load(A, t0, M::k_page(c, b, t0, lane), M::v_page(c, b, t0, lane));
+            int kp = M::k_page(c, b, t0 + JUMP, lane), vp = M::v_page(c, b, t0 + JUMP, lane);
+            auto next = [&](Stage& st) {
+                if (t0 + JUMP < end) {
+                    load(st, t0 + JUMP, kp, vp);
+                    kp = M::k_page(c, b, t0 + 2 * JUMP, lane);
+                    vp = M::v_page(c, b, t0 + 2 * JUMP, lane);
+                }
+            };
+            if constexpr (NC == 1) {
+                Stage B;
+                for (;;) {
+                    next(B);
+                    compute(A, t0);
+                    t0 += JUMP;
+                    if (t0 >= end) break;
+                    next(A);
+                    compute(B, t0);
+                    t0 += JUMP;
+                    if (t0 >= end) break;
+                }
+            } else {
+                for (;;) {
+                    compute(A, t0);
+                    next(A);
+                    t0 += JUMP;
+                    if (t0 >= end) break;
+                }
+            }
+        }
+
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const float sum = row_sum(l[n]);
+            __syncthreads();  // the rows before have been read
+#pragma unroll
+            for (int d = 0; d < DV; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) merge_o[wave][col][DV * (4 * g + e) + d] = acc[n][d][e];
+            if (g == 0) {
+                merge_m[wave][col] = m[n];
+                merge_l[wave][col] = sum;
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < 16 * (D / 4); e += 256) {
+                const int row = e / (D / 4), ch = e % (D / 4) * 4;
+                const int r = (tile * NC + n) * 16 + row;
+                if (r >= rows || ch >= c.d) continue;
+                float top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) top = fmaxf(top, merge_m[w][row]);
+                float x[4] = {}, total = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float mw = merge_m[w][row];
+                    const float f =
+                        mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - top) * c2);
+                    total += f * merge_l[w][row];
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) x[q4] += f * merge_o[w][row][ch + q4];
+                }
+                const bool any = total > 0.f;
+                const float inv = any ? 1.f / total : 0.f;
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] * inv : 0.f;
+                const float lse = any ? fmaf(top, a.scale, __logf(total)) : -INFINITY;
+                const int i = r / G, h = hk * G + r % G;
+                const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
+                if (whole) {
+                    store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch,
+                              a.out_bf16, x);
+                    if (ch == 0 && a.lse) a.lse[at] = lse;
+                } else {
+                    store4(plan.part_o, (at * plan.parts + part) * c.d + ch, false, x);
+                    if (ch == 0) plan.part_lse[at * plan.parts + part] = lse;
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of one (token, head): eight groups of 32 lanes take the parts in
+// turn, four channels a lane, and the groups are added in LDS in their order.
+__global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, const Plan plan,
+                                                          int per_head) {
+    __shared__ float part_x[8][128];
+    __shared__ float part_w[8];
+    const sparsp_cache& c = a.cache;
+    const int bh = blockIdx.x / per_head;
+    const int b = bh / a.q_heads, h = bh % a.q_heads;
+    const Seq s = sequence(c, a.tokens, b);
+    const int keys = part_keys(plan, s.kv);
+    if (s.kv <= keys) return;
+    const int parts = (s.kv + keys - 1) / keys;
+    const int group = threadIdx.x >> 5, ch = (threadIdx.x & 31) * 4;
+    for (int i = blockIdx.x % per_head; i < s.n; i += per_head) {
+        const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
+        const float* lse = plan.part_lse + at * plan.parts;
+        float top = -INFINITY;
+        for (int p = threadIdx.x & 63; p < parts; p += 64) top = fmaxf(top, lse[p]);
+#pragma unroll
+        for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        const float base = top == -INFINITY ? 0.f : top;
+        float x[4] = {}, total = 0.f;
+        for (int p = group; p < parts; p += 8) {
+            const float w = __builtin_amdgcn_exp2f((lse[p] - base) * kLog2e);
+            total += w;
+            if (ch < c.d) {
+                const float4 y =
+                    *reinterpret_cast<const float4*>(plan.part_o + (at * plan.parts + p) * c.d + ch);
+                x[0] += w * y.x;
+                x[1] += w * y.y;
+                x[2] += w * y.z;
+                x[3] += w * y.w;
+            }
+        }
+        __syncthreads();  // the row before has been read
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) part_x[group][ch + q4] = x[q4];
+        if (ch == 0) part_w[group] = total;
+        __syncthreads();
+        if (group == 0) {
+            total = 0.f;
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) x[q4] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                total += part_w[w];
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) x[q4] += part_x[w][ch + q4];
+            }
+            const bool any = total > 0.f;
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] / total : 0.f;
+            if (ch < c.d)
+                store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch,
+                              a.out_bf16, x);
+            if (ch == 0 && a.lse) a.lse[at] = any ? top + __logf(total) : -INFINITY;
+        }
+    }
+}
+
+// The launch for what is known of the lengths. Rows are taken 16 at a time, or 32 where a
+// sequence has more than 16. The keys are split until there are four workgroups per
+// CU, but into parts of at least 512 keys (a part's prologue and merge cost as much as
+// about a hundred keys), and no more than the workspace holds.
+struct Shape {
+    Plan plan;
+    int nc;
+    int64_t bytes;  // of workspace used
+};
+
+Shape shape(const PagedArgs& a, int64_t ws_bytes) {
+    const sparsp_cache& c = a.cache;
+    const int G = a.q_heads / c.H;
+    const int span = c.width * c.page;
+    const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
+    const int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
+    Shape r = {};
+    const int64_t rows = int64_t(most_new) * G;
+    r.nc = rows > 16 ? 2 : 1;
+    int64_t tiles = (rows + 16 * r.nc - 1) / (16 * r.nc);
+    const int64_t pairs = int64_t(c.B) * c.H;
+    const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
+    tiles = std::min(tiles, room);
+    int64_t parts = std::min<int64_t>((most_kv + 511) / 512, 4 * kCus / std::min<int64_t>(pairs * tiles, 4 * kCus));
+    const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
+    parts = std::min(parts, part_bytes > 0 ? ws_bytes / part_bytes : 1);
+    if (parts < 1) parts = 1;
+    r.plan.tiles = int(tiles);
+    r.plan.parts = int(parts);
+    r.plan.step = int(((most_kv + parts - 1) / parts + 127) / 128 * 128);
+    if (r.plan.step < 512) r.plan.step = 512;
+    r.bytes = parts > 1 ? parts * part_bytes : 0;
+    return r;
+}
+
+template <typename T, int D, int NC>
+hipError_t launch_rows(const PagedArgs& a, const Plan& p, hipStream_t s) {
+    const int units = (a.cache.B * a.cache.H * p.parts + 7) / 8 * 8;
+    paged_rows_kernel<T, D, NC><<<units * p.tiles, 256, 0, s>>>(a, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const PagedArgs& a, const Shape& r, hipStream_t s) {
+    if (a.cache.d <= 64)
+        return r.nc == 1 ? launch_rows<T, 64, 1>(a, r.plan, s) : launch_rows<T, 64, 2>(a, r.plan, s);
+    return r.nc == 1 ? launch_rows<T, 128, 1>(a, r.plan, s) : launch_rows<T, 128, 2>(a, r.plan, s);
+}
+
+}  // namespace
+
+int64_t paged_attn_workspace(const PagedArgs& a) {
+    return shape(a, int64_t(1) << 40).bytes;
+}
+
+hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
+    Shape r = shape(a, a.ws ? a.ws_bytes : 0);
+    if (r.plan.parts > 1) {
+        r.plan.part_o = static_cast<float*>(a.ws);
+        r.plan.part_lse = r.plan.part_o + int64_t(a.q_heads) * a.tokens * r.plan.parts * a.cache.d;
+    }
+    hipError_t e = a.cache.dtype == SPARSP_BF16 ? launch_type<uint16_t>(a, r, s)
+                                                : launch_type<float>(a, r, s);
+    if (e != hipSuccess || r.plan.parts == 1) return e;
+    const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
+    const int64_t pairs = int64_t(a.cache.B) * a.q_heads;
+    const int64_t per = std::min<int64_t>(most_new, std::max<int64_t>(1, (int64_t(1) << 22) / pairs));
+    paged_merge_kernel<<<int(pairs * per), 256, 0, s>>>(a, r.plan, int(per));
+    return hipGetLastError();
+}
+
+}  // namespace sparsp

@@ -1,0 +1,389 @@
+"""Binding of the paged cache (include/sparsp_cache.h): argument marshalling only.
+
+    sparsp_rope_frequencies   frequencies of rotary positions, scaled for long contexts (host)
+    sparsp_rope               rotary positions of Q and K, or back
+    sparsp_paged_append       new tokens' K and V into the cache, K and Q rotated on the way
+    sparsp_paged_attn         attention of the new tokens over the cache
+    sparsp_paged_weights      attention weight per cached token
+    sparsp_cache_evict        the cache cut to the tokens of most weight
+
+Token tensors are [heads, tokens, d] with contiguous channels and any other strides: a
+projection's [tokens, heads, d] is passed as x.transpose(0, 1). The cache is K_cache and
+V_cache [pages, H, page, d]; page_table int32 [B, width], new_off int32 [B + 1] and kv_len
+int32 [B] (with the new tokens) describe its sequences. Everything is on one GPU; the calls
+run on that GPU's current stream, or on the stream given.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+import struct
+from dataclasses import dataclass
+from typing import Optional, Sequence
+
+from . import (_SIGNATURES, _RESTYPES, _check, _empty, _stream, _torch, BF16, F32, SparspError,
+               load_library)
+
+__all__ = [
+    "Rotary",
+    "sparsp_rope_frequencies",
+    "sparsp_rope",
+    "sparsp_paged_append",
+    "sparsp_paged_attn",
+    "sparsp_paged_attn_workspace_bytes",
+    "sparsp_paged_weights",
+    "sparsp_cache_evict",
+    "rope_frequencies",
+    "rope",
+    "paged_append",
+    "paged_attn",
+    "paged_attn_workspace_bytes",
+    "paged_weights",
+    "cache_evict",
+]
+
+_VP, _I32, _I64, _F32, _F64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
+                               ctypes.c_double)
+# The structures are packed as bytes, which costs a call less than ctypes fields do.
+_STRUCT = ctypes.c_char_p
+_ROWS = struct.Struct("@Pqqii")
+_ROTARY = struct.Struct("@iiiiiifi")
+_CACHE = struct.Struct("@PPPPPPiiiiiiii")
+
+_SIGNATURES.update({
+    "sparsp_rope_frequencies": [_I32, _F64, _I32, _F64, _F64, _F64, _F64, _VP, _VP],
+    "sparsp_rope": [_STRUCT, _I32, _I32, _I32, _STRUCT, _STRUCT, _I32, _VP, _I32, _VP, _VP],
+    "sparsp_paged_append": [_STRUCT, _I32, _STRUCT, _STRUCT, _STRUCT, _VP, _I32, _VP, _STRUCT,
+                            _STRUCT, _VP],
+    "sparsp_paged_attn": [_STRUCT, _I32, _STRUCT, _STRUCT, _I32, _VP, _I32, _F32, _I32, _I32, _VP,
+                          _I64, _VP],
+    "sparsp_paged_attn_workspace_bytes": [_STRUCT, _I32, _I32, _I32, _I32],
+    "sparsp_paged_weights": [_STRUCT, _I32, _STRUCT, _VP, _I32, _F32, _I32, _I32, _I32, _VP],
+    "sparsp_cache_evict": [_STRUCT, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP],
+})
+_RESTYPES["sparsp_paged_attn_workspace_bytes"] = _I64
+
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """sparsp_rotary: the first rot_dim channels of a row turn in pairs.
+
+    layout "half" pairs channels (p, p + rot_dim/2), "interleaved" (2p, 2p + 1). axis_pairs
+    is the number of pairs that turn with each axis of the positions (None: one axis).
+    """
+
+    rot_dim: int
+    layout: str = "half"
+    axis_pairs: Optional[Sequence[int]] = None
+    factor: float = 1.0
+
+    @property
+    def axes(self) -> int:
+        return 1 if self.axis_pairs is None else len(self.axis_pairs)
+
+    def _pack(self, inverse: bool) -> bytes:
+        if self.layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)} (got {self.layout!r})")
+        pairs = (self.rot_dim // 2,) if self.axis_pairs is None else tuple(self.axis_pairs)
+        if len(pairs) > 3:
+            raise ValueError("at most three axes")
+        a, b, c = pairs + (0,) * (3 - len(pairs))
+        return _ROTARY.pack(self.rot_dim, _LAYOUTS[self.layout], len(pairs), a, b, c, self.factor,
+                            inverse)
+
+
+def _dtype_code(t, name):
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise ValueError(f"{name} must be bfloat16 or float32 (got {t.dtype})")
+
+
+def _on(t, name, device, dtype=None, shape=None):
+    """Address of a contiguous tensor on `device` (None: any GPU)."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU (got {t.device})")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device} (got {t.device})")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+    return t.data_ptr()
+
+
+def _rows(t, name, device, dtype, tokens, d, heads=None):
+    """sparsp_rows of a [heads, tokens, d] tensor."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 3 or not t.is_cuda or t.device != device or t.dtype != dtype:
+        raise ValueError(f"{name} must be a [heads, tokens, d] {dtype} tensor on {device} (got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device})")
+    h, n, c = t.shape
+    if n != tokens or c != d or (heads is not None and h != heads):
+        raise ValueError(f"{name} must have shape {(heads or h, tokens, d)} (got {tuple(t.shape)})")
+    sh, st, sc = t.stride()
+    if sc != 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    # An axis of one entry, or a tensor of none, is never stepped along.
+    if n <= 1 or h <= 1 or not n:
+        sh, st = (sh if h > 1 else d), (st if n > 1 else d)
+    return _ROWS.pack(t.data_ptr() or 16, sh, st, h, 0)
+
+
+def _like_rows(x, dtype=None):
+    """A new tensor in x's order of heads and tokens."""
+    torch = _torch()
+    h, n, d = x.shape
+    if x.stride(1) > x.stride(0):
+        return torch.empty((n, h, d), dtype=dtype or x.dtype, device=x.device).transpose(0, 1)
+    return torch.empty((h, n, d), dtype=dtype or x.dtype, device=x.device)
+
+
+class _On:
+    """The library call with `device` current, which launches need."""
+
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        self.device, self.stream = device, _stream(stream, device)
+
+    def call(self, fn, *args):
+        torch = _torch()
+        if torch._C._cuda_getDevice() == self.device.index:
+            return _check(fn(*args, self.stream))
+        with torch.cuda.device(self.device):
+            return _check(fn(*args, self.stream))
+
+
+def _positions(rotary, positions, inv_freq, tokens, device):
+    torch = _torch()
+    if not isinstance(positions, torch.Tensor):
+        raise TypeError("positions must be a torch.Tensor")
+    if positions.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"positions must be int32 or int64 (got {positions.dtype})")
+    p = positions if positions.dim() == 2 else positions.view(1, -1)
+    return (_on(p, "positions", device, None, (rotary.axes, tokens)) or 16,
+            32 if positions.dtype == torch.int32 else 64,
+            _on(inv_freq, "inv_freq", device, torch.float32, (rotary.rot_dim // 2,)))
+
+
+def sparsp_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "plain",
+                            scale: float = 1.0, trained: float = 0.0, low: float = 1.0,
+                            high: float = 32.0) -> tuple:
+    """Frequencies of rot_dim // 2 pairs (host). Returns (inv_freq float32 numpy, factor).
+
+    scaling: "plain", "linear" (all frequencies over scale), "base" (the base raised so that the
+    lowest frequency is divided by scale) or "parts" (frequencies of fewer than `low` turns over
+    `trained` tokens divided, of more than `high` kept, a ramp between; factor 0.1 ln scale + 1).
+    """
+    import numpy as np
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(_SCALINGS)} (got {scaling!r})")
+    f = np.empty(max(1, int(rot_dim) // 2), dtype=np.float32)
+    factor = ctypes.c_float()
+    _check(load_library().sparsp_rope_frequencies(int(rot_dim), float(theta), _SCALINGS[scaling],
+                                                  float(scale), float(trained), float(low),
+                                                  float(high), f.ctypes.data,
+                                                  ctypes.addressof(factor)))
+    return f, factor.value
+
+
+def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None,
+                inverse: bool = False, stream=None):
+    """X [heads, tokens, d] rotated to positions [axes, tokens] (or [tokens]); X2 alike.
+
+    Returns Y, or (Y, Y2) with X2. Y may be X (in place). With inverse the transposed rotation:
+    it turns back (times factor squared), and carries a gradient of Y to one of X.
+    """
+    torch = _torch()
+    if not isinstance(X, torch.Tensor):
+        raise TypeError("X must be a torch.Tensor")
+    code = _dtype_code(X, "X")
+    if X.dim() != 3 or not X.is_cuda:
+        raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
+    dev, (_, n, d) = X.device, X.shape
+    on = _On(dev, stream)
+    y = Y if Y is not None else _like_rows(X)
+    x, o, count = _rows(X, "X", dev, X.dtype, n, d), _rows(y, "Y", dev, X.dtype, n, d, X.shape[0]), 1
+    y2 = None
+    if X2 is not None:
+        x += _rows(X2, "X2", dev, X.dtype, n, d)
+        y2 = Y2 if Y2 is not None else _like_rows(X2)
+        o += _rows(y2, "Y2", dev, X.dtype, n, d, X2.shape[0])
+        count = 2
+    elif Y2 is not None:
+        raise ValueError("Y2 needs X2")
+    pos, bits, freq = _positions(rotary, positions, inv_freq, n, dev)
+    on.call(load_library().sparsp_rope, rotary._pack(inverse), n, d, code, x, o, count, pos, bits,
+            freq)
+    return y if X2 is None else (y, y2)
+
+
+def _cache(K_cache, V_cache, weights, page_table, new_off, kv_len):
+    """(sparsp_cache, device) of the cache's tensors; V_cache, weights, new_off may be None."""
+    torch = _torch()
+    if not isinstance(K_cache, torch.Tensor):
+        raise TypeError("K_cache must be a torch.Tensor")
+    if K_cache.dim() != 4:
+        raise ValueError("K_cache must be [pages, H, page, d]")
+    dev, shape, i32 = K_cache.device, K_cache.shape, torch.int32
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an int32 [B, width] tensor")
+    B, width = page_table.shape
+    k = _on(K_cache, "K_cache", None)
+    v = 0 if V_cache is None else _on(V_cache, "V_cache", dev, K_cache.dtype, shape)
+    w = 0 if weights is None else _on(weights, "weights", dev, torch.float32, shape[:3])
+    return _CACHE.pack(
+        k, v, w, _on(page_table, "page_table", dev, i32),
+        0 if new_off is None else _on(new_off, "new_off", dev, i32, (B + 1,)),
+        _on(kv_len, "kv_len", dev, i32, (B,)), shape[0], shape[1], shape[2], shape[3],
+        _dtype_code(K_cache, "K_cache"), width, B, 0), dev
+
+
+def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, weights=None,
+                        rotary: Optional[Rotary] = None, positions=None, inv_freq=None, Q=None,
+                        Q_out=None, stream=None):
+    """Writes the new tokens' K, V [H, tokens, d] into the cache (and 0 into their weights, if given).
+
+    With a rotation K is rotated to its positions on the way, and so is Q, into Q_out (which may
+    be Q). Returns Q_out, or None without Q.
+    """
+    c, dev = _cache(K_cache, V_cache, weights, page_table, new_off, kv_len)
+    on = _On(dev, stream)
+    if K.dim() != 3:
+        raise ValueError("K must be [H, tokens, d]")
+    H, n, d, dt = K_cache.shape[1], K.shape[1], K_cache.shape[3], K_cache.dtype
+    rot, pos, bits, freq, q, qo = None, None, 32, None, None, None
+    if rotary is not None:
+        rot = rotary._pack(False)
+        pos, bits, freq = _positions(rotary, positions, inv_freq, n, dev)
+    if Q is not None:
+        q = _rows(Q, "Q", dev, dt, n, d)
+        if Q_out is None:
+            Q_out = _like_rows(Q)
+        qo = _rows(Q_out, "Q_out", dev, dt, n, d, Q.shape[0])
+    elif Q_out is not None:
+        raise ValueError("Q_out needs Q")
+    on.call(load_library().sparsp_paged_append, c, n, _rows(K, "K", dev, dt, n, d, H),
+            _rows(V, "V", dev, dt, n, d, H), rot, pos, bits, freq, q, qo)
+    return Q_out
+
+
+def sparsp_paged_attn_workspace_bytes(K_cache, page_table, tokens: int, q_heads: int,
+                                      max_new: int = 0, max_kv: int = 0) -> int:
+    """Workspace bytes that sparsp_paged_attn can use for these shapes (host)."""
+    B, width = page_table.shape
+    P, H, page, d = K_cache.shape
+    c = _CACHE.pack(0, 0, 0, 0, 0, 0, P, H, page, d, _dtype_code(K_cache, "K_cache"), width, B, 0)
+    n = int(load_library().sparsp_paged_attn_workspace_bytes(c, int(tokens), int(q_heads),
+                                                            int(max_new or 0), int(max_kv or 0)))
+    _check(n if n < 0 else 0)
+    return n
+
+
+def _scale(softmax_scale, d):
+    return 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale)
+
+
+def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: bool = True,
+                      softmax_scale: Optional[float] = None, max_new: Optional[int] = None,
+                      max_kv: Optional[int] = None, O=None, lse=None, want_lse: bool = True,
+                      out_dtype: Optional[int] = None, workspace=None, stream=None):
+    """Attention of the new tokens Q [heads, tokens, d] over the cache. Returns (O, lse or None).
+
+    O is [heads, tokens, d] (contiguous unless given), lse float32 [heads, tokens]. max_new and
+    max_kv, the largest numbers of new and of cached tokens if the caller knows them, size the
+    launch. With workspace (any device tensor, e.g. of sparsp_paged_attn_workspace_bytes bytes)
+    long caches are split among workgroups; without, one workgroup walks a sequence's keys.
+    """
+    torch = _torch()
+    c, dev = _cache(K_cache, V_cache, None, page_table, new_off, kv_len)
+    on = _On(dev, stream)
+    d, dt = K_cache.shape[3], K_cache.dtype
+    if Q.dim() != 3:
+        raise ValueError("Q must be [heads, tokens, d]")
+    heads, n = Q.shape[0], Q.shape[1]
+    if out_dtype is None:
+        out_dtype = _dtype_code(K_cache, "K_cache")
+    odt = torch.bfloat16 if out_dtype == BF16 else torch.float32
+    o = O if O is not None else _empty((heads, n, d), odt, Q)
+    ls = lse if lse is not None else _empty((heads, n), torch.float32, Q) if want_lse else None
+    ws, nbytes = None, 0
+    if workspace is not None:
+        ws = _on(workspace, "workspace", dev)
+        nbytes = workspace.numel() * workspace.element_size()
+    on.call(load_library().sparsp_paged_attn, c, n, _rows(Q, "Q", dev, dt, n, d),
+            _rows(o, "O", dev, odt, n, d, heads), int(out_dtype),
+            None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
+            bool(causal), _scale(softmax_scale, d), int(max_new or 0), int(max_kv or 0), ws, nbytes)
+    return o, ls
+
+
+def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
+                         causal: bool = True, softmax_scale: Optional[float] = None,
+                         accumulate: bool = True, max_new: Optional[int] = None,
+                         max_kv: Optional[int] = None, stream=None):
+    """Adds (or with accumulate=False writes) the attention weight of every cached token.
+
+    Q, lse and the other arguments as given to and returned by sparsp_paged_attn; weights
+    float32 [pages, H, page]. Returns weights.
+    """
+    torch = _torch()
+    c, dev = _cache(K_cache, None, weights, page_table, new_off, kv_len)
+    on = _On(dev, stream)
+    if Q.dim() != 3:
+        raise ValueError("Q must be [heads, tokens, d]")
+    heads, n, d = Q.shape
+    if d != K_cache.shape[3]:
+        raise ValueError(f"Q must have d = {K_cache.shape[3]} (got {d})")
+    if weights is None:
+        raise TypeError("weights must be a torch.Tensor")
+    on.call(load_library().sparsp_paged_weights, c, n, _rows(Q, "Q", dev, K_cache.dtype, n, d),
+            _on(lse, "lse", dev, torch.float32, (heads, n)) or 16, bool(causal),
+            _scale(softmax_scale, d), bool(accumulate), int(max_new or 0), int(max_kv or 0))
+    return weights
+
+
+def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int, first: int = 0,
+                       recent: int = 0, dst_table=None, kv_len_out=None, kept=None, stream=None):
+    """Cuts every sequence of more than `keep` tokens to `keep`: its first and recent ones, and
+    of the others, per head, those of most weight. Returns (kv_len_out [B], kept [B, H, keep]).
+
+    The kept tokens move to the front of the sequence's pages, or into the pages of dst_table
+    (int32 [B, width], none of them in page_table). kept lists them, ascending, then -1.
+    """
+    torch = _torch()
+    c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
+    on = _On(dev, stream)
+    B, H, keep = page_table.shape[0], K_cache.shape[1], int(keep)
+    out = kv_len_out if kv_len_out is not None else torch.empty_like(kv_len)
+    lst = kept if kept is not None else _empty((B, H, max(keep, 0)), torch.int32, K_cache)
+    dst, dst_width = None, 0
+    if dst_table is not None:
+        if dst_table.dim() != 2 or dst_table.shape[0] != B:
+            raise ValueError(f"dst_table must be an int32 [{B}, width] tensor")
+        dst, dst_width = _on(dst_table, "dst_table", dev, torch.int32), dst_table.shape[1]
+    on.call(load_library().sparsp_cache_evict, c, keep, int(first), int(recent), dst, dst_width,
+            _on(out, "kv_len_out", dev, torch.int32, (B,)),
+            _on(lst, "kept", dev, torch.int32, (B, H, max(keep, 0))))
+    return out, lst
+
+
+rope_frequencies = sparsp_rope_frequencies
+rope = sparsp_rope
+paged_append = sparsp_paged_append
+paged_attn = sparsp_paged_attn
+paged_attn_workspace_bytes = sparsp_paged_attn_workspace_bytes
+paged_weights = sparsp_paged_weights
+cache_evict = sparsp_cache_evict
