@@ -57,10 +57,10 @@ COMMON = [
 ]
 
 
-# Extra flags per source. The bf16 attention kernel never sees NaN (inputs are
+# Extra flags per source. The bf16 attention kernels never see NaN (inputs are
 # finite, masked keys are -inf), so fmaxf needs no NaN quieting; infinities are
 # still honoured.
-PER_FILE = {"attn_bf16.hip": ["-fno-honor-nans"]}
+PER_FILE = {"attn_bf16.hip": ["-fno-honor-nans"], "paged_attn_tiles.hip": ["-fno-honor-nans"]}
 
 
 def hipcc() -> str:

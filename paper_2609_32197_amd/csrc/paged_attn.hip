@@ -15,6 +15,7 @@
 // their order. A sequence short enough for one part writes its output directly.
 #include <algorithm>
 
+#include "paged_plan.h"
 #include "paged_tiles.h"
 
 namespace sparsp {
@@ -22,36 +23,8 @@ namespace {
 
 constexpr int kCus = 256;
 
-// The launch's view of the work: `tiles` workgroups stride over a sequence's row tiles,
-// `parts` over its keys.
-struct Plan {
-    int tiles, parts, step;
-    float* part_o;    // [q_heads, tokens, parts, d]
-    float* part_lse;  // [q_heads, tokens, parts]
-};
-
-// Keys of a part of a sequence of kv cached tokens: a multiple of step, so many that
-// `parts` of them cover kv.
-__device__ __forceinline__ int part_keys(const Plan& p, int kv) {
-    const int64_t all = (int64_t(kv) + p.parts - 1) / p.parts;
-    const int64_t k = (all + p.step - 1) / p.step * p.step;
-    return int(k < p.step ? p.step : k);
-}
-
-__device__ __forceinline__ void store4(void* O, int64_t at, bool bf16, const float (&x)[4]) {
-    if (bf16) {
-        uint2 w;
-        w.x = f32_to_bf16_bits(x[0]) | (f32_to_bf16_bits(x[1]) << 16);
-        w.y = f32_to_bf16_bits(x[2]) | (f32_to_bf16_bits(x[3]) << 16);
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(O) + at) = w;
-    } else {
-        *reinterpret_cast<float4*>(static_cast<float*>(O) + at) =
-            make_float4(x[0], x[1], x[2], x[3]);
-    }
-}
-
 template <typename T, int D, int NC>
-__global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, const Plan plan) {
+__global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, const PagedPlan plan) {
     using M = TileMath<T, D>;
     constexpr int KEYS = M::KEYS, DV = M::DV, PITCH = D + 4;
     __shared__ float merge_o[4][16][PITCH];
@@ -255,7 +228,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
 
 // Joins the parts of one (token, head): eight groups of 32 lanes take the parts in
 // turn, four channels a lane, and the groups are added in LDS in their order.
-__global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, const Plan plan,
+__global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, const PagedPlan plan,
                                                           int per_head) {
     __shared__ float part_x[8][128];
     __shared__ float part_w[8];
@@ -314,13 +287,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     }
 }
 
-// The launch for what is known of the lengths. Rows are taken 16 at a time, or 32 where a
-// sequence has more than 16. The keys are split until there are four workgroups per
-// CU, but into parts of at least 512 keys (a part's prologue and merge cost as much as
-// about a hundred keys), and no more than the workspace holds.
+// The launch for what is known of the lengths. bf16 rows of more than 32 a sequence go to
+// the kernel of 128-row tiles; others are taken 16 at a time, or 32 where there are more than
+// 16. The keys are split until there are four workgroups per CU, but into parts of at
+// least 512 keys (a part's prologue and merge cost as much as about a hundred keys), and no
+// more than the workspace holds.
 struct Shape {
-    Plan plan;
-    int nc;
+    PagedPlan plan;
+    int rows;       // of a tile
     int64_t bytes;  // of workspace used
 };
 
@@ -332,25 +306,24 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
     Shape r = {};
     const int64_t rows = int64_t(most_new) * G;
-    r.nc = rows > 16 ? 2 : 1;
-    int64_t tiles = (rows + 16 * r.nc - 1) / (16 * r.nc);
+    r.rows = rows <= 16 ? 16 : rows <= 32 || c.dtype == SPARSP_F32 ? 32 : 128;
+    int64_t tiles = (rows + r.rows - 1) / r.rows;
     const int64_t pairs = int64_t(c.B) * c.H;
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
     tiles = std::min(tiles, room);
-    int64_t parts = std::min<int64_t>((most_kv + 511) / 512, 4 * kCus / std::min<int64_t>(pairs * tiles, 4 * kCus));
+    int64_t parts = std::min<int64_t>((most_kv + 511) / 512,
+                                      4 * kCus / std::min<int64_t>(pairs * tiles, 4 * kCus));
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
-    parts = std::min(parts, part_bytes > 0 ? ws_bytes / part_bytes : 1);
-    if (parts < 1) parts = 1;
+    parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);
-    r.plan.step = int(((most_kv + parts - 1) / parts + 127) / 128 * 128);
-    if (r.plan.step < 512) r.plan.step = 512;
+    r.plan.step = std::max(512, int(((most_kv + parts - 1) / parts + 127) / 128 * 128));
     r.bytes = parts > 1 ? parts * part_bytes : 0;
     return r;
 }
 
 template <typename T, int D, int NC>
-hipError_t launch_rows(const PagedArgs& a, const Plan& p, hipStream_t s) {
+hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
     const int units = (a.cache.B * a.cache.H * p.parts + 7) / 8 * 8;
     paged_rows_kernel<T, D, NC><<<units * p.tiles, 256, 0, s>>>(a, p);
     return hipGetLastError();
@@ -359,8 +332,10 @@ hipError_t launch_rows(const PagedArgs& a, const Plan& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_type(const PagedArgs& a, const Shape& r, hipStream_t s) {
     if (a.cache.d <= 64)
-        return r.nc == 1 ? launch_rows<T, 64, 1>(a, r.plan, s) : launch_rows<T, 64, 2>(a, r.plan, s);
-    return r.nc == 1 ? launch_rows<T, 128, 1>(a, r.plan, s) : launch_rows<T, 128, 2>(a, r.plan, s);
+        return r.rows == 16 ? launch_rows<T, 64, 1>(a, r.plan, s)
+                            : launch_rows<T, 64, 2>(a, r.plan, s);
+    return r.rows == 16 ? launch_rows<T, 128, 1>(a, r.plan, s)
+                        : launch_rows<T, 128, 2>(a, r.plan, s);
 }
 
 }  // namespace
@@ -375,8 +350,9 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
         r.plan.part_o = static_cast<float*>(a.ws);
         r.plan.part_lse = r.plan.part_o + int64_t(a.q_heads) * a.tokens * r.plan.parts * a.cache.d;
     }
-    hipError_t e = a.cache.dtype == SPARSP_BF16 ? launch_type<uint16_t>(a, r, s)
-                                                : launch_type<float>(a, r, s);
+    hipError_t e = r.rows == 128                   ? launch_paged_tiles(a, r.plan, s)
+                   : a.cache.dtype == SPARSP_BF16 ? launch_type<uint16_t>(a, r, s)
+                                                  : launch_type<float>(a, r, s);
     if (e != hipSuccess || r.plan.parts == 1) return e;
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
     const int64_t pairs = int64_t(a.cache.B) * a.q_heads;

@@ -1,0 +1,378 @@
+// Attention of many new tokens over the paged cache, bf16: 128 rows (token, head of the
+// group) a workgroup, K and V tiles of 64 keys shared by its four waves through LDS.
+//
+// Each wave owns 32 rows against every key and runs one online softmax. Score and output
+// tiles are computed transposed with v_mfma_f32_16x16x32_bf16, S^T = K Q^T and O^T = V^T P^T,
+// and the keys are dealt to the rows of the score tiles so that a lane's probabilities are its
+// operand of the second product (the layout is stated in paged_tiles.h; a wave's two column
+// groups of 16 rows share every operand of K and V). V lies in LDS as it lies in the cache,
+// one key a row; its transposed operand comes from ds_read_b64_tr_b16: in a group of 16
+// lanes, lane i points at 4 channels of key i / 4, channels 4 (i % 4), and receives channel
+// i of the four keys. Two such reads make the eight keys of an operand.
+//
+// Tiles are double-buffered: the copies of tile j+1 are issued right after the barrier that
+// opens tile j. They are direct-to-LDS buffer loads; one instruction of a wave copies 1 KB,
+// 4 rows of 128 channels or 8 of 64, which lie on one page, through a descriptor rooted at
+// that row of the page and ending with the sequence: rows behind it, rows of a page that
+// does not exist and channels behind d become zeros. The page numbers of the next 16,384 keys
+// are held in LDS, since a load of them in the loop would wait for the copies.
+//
+// Swizzle: 16-byte chunks of an LDS row are exchanged by an XOR with bits of the row, applied to
+// the source addresses of the copies. K rows read together by 16 lanes (8 i + j + const,
+// i, j < 4) land on their own 16 bytes of 256; V rows read together by 32 lanes (8 i + j +
+// const, i < 2, j < 4) on their own 32 bytes.
+#include <type_traits>
+
+#include "paged_plan.h"
+
+namespace sparsp {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+constexpr int kKeys = 64;        // keys of a tile
+constexpr int kRowsTile = 128;   // rows of a workgroup
+constexpr int kSegment = 16384;  // keys whose page numbers are held at once
+
+// Max and sum over the four lanes that hold a row.
+__device__ __forceinline__ float quad_max(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The XOR of a row's 16-byte chunk number, for K and for V.
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row) {
+    const int i = (row >> 3) & 3;
+    return D == 128 ? (row & 3) | (i << 2) : ((row >> 1) & 1) | (i << 1);
+}
+template <int D>
+__device__ __forceinline__ int v_swizzle(int row) {
+    const int i = (row >> 3) & 1;
+    return (D == 128 ? (row & 3) | (i << 2) : ((row >> 1) & 1) | (i << 1)) << 1;
+}
+
+// One 1 KB copy of K and one of V to LDS. Inline assembly, because the compiler would guard
+// every later LDS read with a wait for all copies in flight; the waits are explicit. M0 is
+// restored, and a wait state separates each write of it from its use.
+__device__ __forceinline__ void copy_pair(const u32x4_t& kd, const u32x4_t& vd, int koff, int voff,
+                                          uint32_t k_lds, uint32_t v_lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %[sv], m0\n\t"
+        "s_mov_b32 m0, %[kl]\n\ts_nop 0\n\t"
+        "buffer_load_dwordx4 %[ko], %[kd], 0 offen lds\n\t"
+        "s_mov_b32 m0, %[vl]\n\ts_nop 0\n\t"
+        "buffer_load_dwordx4 %[vo], %[vd], 0 offen lds\n\t"
+        "s_mov_b32 m0, %[sv]"
+        : [sv] "=&s"(saved)
+        : [kl] "s"(k_lds), [vl] "s"(v_lds), [kd] "s"(kd), [vd] "s"(vd), [ko] "v"(koff),
+          [vo] "v"(voff)
+        : "memory");
+#endif
+}
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
+    constexpr int TILE = kKeys * D;
+    constexpr int NCH = D / 8;         // 16-byte chunks of a row
+    constexpr int RPI = 64 / NCH;      // rows of one copy instruction
+    constexpr int NI = kKeys / 4 / RPI;  // copy instructions of a wave, each of K and V
+    constexpr int KT = D / 32, DT = D / 16;
+    __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];  // [buffer][K, V]
+    __shared__ int page_list[kSegment / 16];
+
+    const sparsp_cache& c = a.cache;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    // The row tiles of one part of the keys run on one XCD, one after another.
+    const int units = c.B * c.H * plan.parts;
+    const int turn = blockIdx.x >> 3;
+    const int unit = turn / plan.tiles * 8 + (blockIdx.x & 7);
+    if (unit >= units) return;
+    const int part = unit % plan.parts, bh = unit / plan.parts;
+    const int b = bh / c.H, hk = bh % c.H;
+    const int G = a.q_heads / c.H;
+    const Seq s = sequence(c, a.tokens, b);
+    const int rows = s.n * G;
+    const int keys = part_keys(plan, s.kv);
+    const bool whole = s.kv <= keys;
+    if (part > 0 && part * int64_t(keys) >= s.kv) return;
+    const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
+    const float c2 = a.scale * kLog2e;
+    const int shift = __builtin_ctz(c.page);
+    const uint32_t row_bytes = uint32_t(c.d) * 2;
+
+    // Source offsets of this lane's copies within an instruction's rows; channels behind d lie
+    // past every descriptor.
+    int koff[NI], voff[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+        const int sub = lane / NCH, row = (n * 4 + wave) * RPI + sub, pc = lane % NCH;
+        const int kc = (pc ^ k_swizzle<D>(row)) * 8, vc = (pc ^ v_swizzle<D>(row)) * 8;
+        koff[n] = kc < c.d ? int(sub * row_bytes) + kc * 2 : 0x7ffffff0;
+        voff[n] = vc < c.d ? int(sub * row_bytes) + vc * 2 : 0x7ffffff0;
+    }
+    // Byte addresses of this lane's operands in a tile: the XOR with kt (dt) and the immediate
+    // offsets of a tile's other rows are added where they are read.
+    const int krow = 8 * (col >> 2) + (col & 3);
+    const uint32_t k_at = uint32_t(krow * D * 2 + ((g ^ k_swizzle<D>(krow)) * 16));
+    const int vrow = 8 * g + (col >> 2);
+    const uint32_t v_at = uint32_t(vrow * D * 2 + (((col & 3) >> 1) ^ v_swizzle<D>(vrow)) * 16 +
+                                   (col & 1) * 8);
+
+    // Later row tiles see more keys: they come first.
+    for (int turns = turn % plan.tiles; turns * int64_t(kRowsTile) < rows; turns += plan.tiles) {
+        const int n_tiles = (rows + kRowsTile - 1) / kRowsTile;
+        const int tile = n_tiles - 1 - turns;
+        bf16x8 q[2][KT];
+        int limit[2], lowest = 1 << 30, highest = 0;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int r = tile * kRowsTile + wave * 32 + n * 16 + col;
+            const bool live = r < rows;
+            const int i = live ? r / G : 0, h = hk * G + (live ? r % G : 0);
+            limit[n] = !live ? 0 : a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+            if (live) lowest = min(lowest, limit[n]);
+            highest = max(highest, limit[n]);
+            const uint16_t* p = static_cast<const uint16_t*>(a.Q) + int64_t(h) * a.q_head +
+                                int64_t(s.q0 + i) * a.q_token;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const int ch = 32 * kt + 8 * g;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (live && ch < c.d) x = *reinterpret_cast<const uint4*>(p + ch);
+                q[n][kt] = __builtin_bit_cast(bf16x8, x);
+            }
+        }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) {
+            lowest = min(lowest, __shfl_xor(lowest, off));
+            highest = max(highest, __shfl_xor(highest, off));
+        }
+        lowest = __builtin_amdgcn_readfirstlane(min(lowest, part_end));
+        highest = __builtin_amdgcn_readfirstlane(min(highest, part_end));
+        const int last = min(rows, (tile + 1) * kRowsTile) - 1;
+        const int end = min(a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv, part_end);
+
+        floatx4 acc[2][DT];
+        float m[2], l[2], lim[2], base[2];  // running max (log2 units), mass, see below
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            m[n] = lim[n] = -INFINITY;
+            l[n] = base[n] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[n][dt] = floatx4{};
+        }
+
+        for (int seg = lo; seg < end; seg += kSegment) {
+            const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
+            __syncthreads();  // the list and the tiles of the segment before have been read
+            int bad = 0;
+            for (int e = tid; e < ((((seg_end + kKeys - 1) & -kKeys) - 1) >> shift) - p0 + 1;
+                 e += 256) {
+                const int p = page_of(c.table, c.width, c.pages, b, p0 + e);
+                page_list[e] = p;
+                bad |= p < 0 && (p0 + e) << shift < seg_end;
+            }
+            bad = __syncthreads_or(bad);
+
+            auto issue = [&](int t0, auto buf_c) {
+                constexpr int buf = decltype(buf_c)::value;
+#pragma unroll
+                for (int n = 0; n < NI; ++n) {
+                    const int r0 = (n * 4 + wave) * RPI, key = t0 + r0;
+                    const int p = __builtin_amdgcn_readfirstlane(page_list[(key >> shift) - p0]);
+                    const int live = p < 0 ? 0 : min(max(s.kv - key, 0), RPI);
+                    const uint64_t row = (uint64_t(uint32_t(max(p, 0))) * uint32_t(c.H) + hk) * c.page +
+                                         (key & (c.page - 1));
+                    const uint64_t k_from = reinterpret_cast<uint64_t>(c.K) + row * row_bytes;
+                    const uint64_t v_from = reinterpret_cast<uint64_t>(c.V) + row * row_bytes;
+                    u32x4_t kd, vd;
+                    kd.x = __builtin_amdgcn_readfirstlane(uint32_t(k_from));
+                    kd.y = __builtin_amdgcn_readfirstlane(uint32_t(k_from >> 32) & 0xffffu);
+                    vd.x = __builtin_amdgcn_readfirstlane(uint32_t(v_from));
+                    vd.y = __builtin_amdgcn_readfirstlane(uint32_t(v_from >> 32) & 0xffffu);
+                    kd.z = vd.z = __builtin_amdgcn_readfirstlane(uint32_t(live) * row_bytes);
+                    kd.w = vd.w = 0x00020000u;
+                    copy_pair(kd, vd, koff[n], voff[n],
+                              __builtin_amdgcn_readfirstlane(
+                                  uint32_t(reinterpret_cast<uintptr_t>(&lds[buf][0][r0 * D]))),
+                              __builtin_amdgcn_readfirstlane(
+                                  uint32_t(reinterpret_cast<uintptr_t>(&lds[buf][1][r0 * D]))));
+                }
+            };
+
+            auto step = [&](int t0, auto buf_c) {
+                constexpr int buf = decltype(buf_c)::value;
+                // Each wave waits for its own copies; the barrier then publishes the tile, and
+                // everyone is done with the one before.
+                __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+                __syncthreads();
+                if (t0 + kKeys < seg_end) issue(t0 + kKeys, std::integral_constant<int, buf ^ 1>{});
+                if (t0 >= highest) return;  // no row of this wave sees any of it
+
+                const char* lk = reinterpret_cast<const char*>(&lds[buf][0][0]);
+                const char* lv = reinterpret_cast<const char*>(&lds[buf][1][0]);
+                // s[n][mt][e]: key 32 (mt/2) + 8 g + 4 (mt%2) + e of column group n's row `col`.
+                floatx4 sc[2][4];
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) sc[0][mt] = sc[1][mt] = floatx4{};
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    bf16x8 ka[4];
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt)
+                        ka[mt] = *reinterpret_cast<const bf16x8*>(
+                            lk + (k_at ^ (kt << 6)) + (32 * (mt >> 1) + 4 * (mt & 1)) * D * 2);
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            sc[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[mt], q[n][kt],
+                                                                                sc[n][mt], 0, 0, 0);
+                }
+                auto v_operand = [&](int t, int dt) {
+                    const char* p = lv + (v_at ^ (dt << 5)) + 32 * t * D * 2;
+                    const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p));
+                    const short4_t y =
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * D * 2));
+                    const short8_t z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                    return __builtin_bit_cast(bf16x8, z);
+                };
+
+                if (bad || t0 + kKeys > lowest) {
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt) {
+                        const int key = t0 + 32 * (mt >> 1) + 8 * g + 4 * (mt & 1);
+                        const bool gone = bad && page_list[(key >> shift) - p0] < 0;
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (gone || key + e >= min(limit[n], part_end))
+                                    sc[n][mt][e] = -INFINITY;
+                    }
+                }
+                // The running max moves where a row's new max carries more than a quarter of
+                // the mass so far (it then enters as exactly 1, which bf16 holds), or more than
+                // 2^8 of it: on spread rows most tiles leave it.
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2)
+                            mx = fmaxf(fmaxf(mx, sc[n][mt][e]), sc[n][mt][e + 1]);
+                    mx = quad_max(mx) * c2;
+                    if (__ballot(mx > lim[n]) != 0) {
+                        const float top = fmaxf(m[n], mx);
+                        const float alpha =
+                            top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
+                        m[n] = top;
+                        l[n] *= alpha;
+                        lim[n] = top + fminf(8.f, fmaxf(0.f, __log2f(l[n]) - 2.f));
+                        base[n] = top == -INFINITY ? 0.f : -top;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) acc[n][dt] *= alpha;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bf16x8 pb[2];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        floatx8 p;
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) {
+                            p[v] = __builtin_amdgcn_exp2f(
+                                fmaf(sc[n][2 * t + v / 4][v % 4], c2, base[n]));
+                            l[n] += p[v];
+                        }
+                        pb[n] = __builtin_convertvector(p, bf16x8);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const bf16x8 va = v_operand(t, dt);
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n],
+                                                                                 acc[n][dt], 0, 0, 0);
+                    }
+                }
+            };
+
+            issue(seg, std::integral_constant<int, 0>{});
+            for (int t0 = seg; t0 < seg_end; t0 += 2 * kKeys) {
+                step(t0, std::integral_constant<int, 0>{});
+                if (t0 + kKeys < seg_end) step(t0 + kKeys, std::integral_constant<int, 1>{});
+            }
+        }
+
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int r = tile * kRowsTile + wave * 32 + n * 16 + col;
+            const float total = quad_sum(l[n]);
+            if (r >= rows) continue;
+            const int i = r / G, h = hk * G + r % G;
+            const bool any = total > 0.f;
+            const float inv = any ? 1.f / total : 0.f;
+            const float lse = any ? (m[n] + __log2f(total)) * kLn2 : -INFINITY;
+            const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
+            const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
+                                     : (at * plan.parts + part) * c.d;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const int ch = 16 * dt + 4 * g;
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = any ? acc[n][dt][e] * inv : 0.f;
+                if (ch >= c.d) continue;
+                if (whole)
+                    store4(a.O, to + ch, a.out_bf16, x);
+                else
+                    store4(plan.part_o, to + ch, false, x);
+            }
+            if (g == 0) {
+                if (!whole)
+                    plan.part_lse[at * plan.parts + part] = lse;
+                else if (a.lse)
+                    a.lse[at] = lse;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
+    const int units = (a.cache.B * a.cache.H * p.parts + 7) / 8 * 8;
+    if (a.cache.d <= 64)
+        paged_tiles_kernel<64><<<units * p.tiles, 256, 0, s>>>(a, p);
+    else
+        paged_tiles_kernel<128><<<units * p.tiles, 256, 0, s>>>(a, p);
+    return hipGetLastError();
+}
+
+}  // namespace sparsp

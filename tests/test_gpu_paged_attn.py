@@ -84,6 +84,13 @@ def test_split_keys(gpu, dtype, new, kv):
         assert (ws[nbytes:] == 255).all()
 
 
+@pytest.mark.parametrize("d,page,bad", [(64, 16, ()), (128, 256, ((0, 3), (0, 64), (0, 80)))])
+def test_long_cache_without_workspace(gpu, d, page, bad):
+    """More keys than one list of page numbers holds, and a last tile of one key."""
+    bt = R.Batch(33, BF, 1, 1, d, page, (50,), (2 * 16384 + 1,), bad=bad)
+    check(bt, *run(bt, workspace=False), causal=True)
+
+
 def test_hints_only_size_the_launch(gpu):
     """Hints below the truth, above it, and none: right every time."""
     bt = R.Batch(23, BF, 4, 2, 64, 16, (90, 1, 35), (2100, 600, 40))
