@@ -26,4 +26,16 @@ __device__ __forceinline__ int page_of(const int32_t* table, int width, int page
     return p >= 0 && p < pages ? p : -1;
 }
 
+// x / d for 0 <= x < 2^31 by one multiplication: m = floor(2^32 / d) + 1 is exact while
+// x * d < 2^32; a step corrects larger x.
+struct Div {
+    uint32_t d, m;
+    __device__ __forceinline__ uint32_t quot(uint32_t x) const {
+        uint32_t q = d == 1 ? x : __umulhi(x, m);
+        if (q * d > x) --q;
+        return q;
+    }
+};
+inline Div make_div(uint32_t d) { return {d, uint32_t((uint64_t(1) << 32) / d) + 1}; }
+
 }  // namespace sparsp

@@ -4,6 +4,7 @@
 // 16 at a time; each lane sums the exponentials of its keys over its column of rows,
 // and the sixteen columns are added once at the end. No two waves add to the same
 // weight, so there are no atomics and the order of a sum depends on the sizes alone.
+#include "paged_plan.h"
 #include "paged_tiles.h"
 
 namespace sparsp {
@@ -86,6 +87,9 @@ hipError_t launch_t(const PagedArgs& a, int strides, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_paged_weights(const PagedArgs& a, hipStream_t s) {
+    const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
+    if (a.cache.dtype == SPARSP_BF16 && int64_t(most_new) * (a.q_heads / a.cache.H) > 32)
+        return launch_weights_tiles(a, s);
     const int span = a.cache.width * a.cache.page;
     const int keys = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
     const int per = 4 * (a.cache.dtype == SPARSP_BF16 ? 32 : 16);

@@ -20,18 +20,6 @@ constexpr int kThreads = 256;
 constexpr int kMaxPer = 16;         // tokens of a workgroup at most
 constexpr int kTableFloats = 2048;  // float2 entries of cos and sin
 
-// x / d for 0 <= x < 2^31 by one multiplication: m = floor(2^32 / d) + 1 is exact while
-// x * d < 2^32; a step corrects larger x.
-struct Div {
-    uint32_t d, m;
-    __device__ __forceinline__ uint32_t quot(uint32_t x) const {
-        uint32_t q = d == 1 ? x : __umulhi(x, m);
-        if (q * d > x) --q;
-        return q;
-    }
-};
-Div make_div(uint32_t d) { return {d, uint32_t((uint64_t(1) << 32) / d) + 1}; }
-
 struct Move {
     const char* src;
     int64_t src_head, src_token;  // bytes
