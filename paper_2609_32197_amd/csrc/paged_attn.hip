@@ -22,6 +22,7 @@ namespace sparsp {
 namespace {
 
 constexpr int kCus = 256;
+constexpr int kSegment = 16384;  // keys whose page numbers are held at once
 
 template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, const PagedPlan plan) {
@@ -29,6 +30,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     constexpr int KEYS = M::KEYS, DV = M::DV, PITCH = D + 4;
     __shared__ float merge_o[4][16][PITCH];
     __shared__ float merge_m[4][16], merge_l[4][16];
+    __shared__ int page_list[kSegment / 16];
     const sparsp_cache& c = a.cache;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, g = lane >> 4;
@@ -38,7 +40,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
     const int unit = k / plan.tiles * 8 + xcd;
     if (unit >= units) return;
-    const int part = unit % plan.parts, bh = unit / plan.parts;
+    const auto [bh, part] = unit_of(unit, c.B * c.H);
     const int b = bh / c.H, hk = bh % c.H;
     const int G = a.q_heads / c.H;
     const Seq s = sequence(c, a.tokens, b);
@@ -48,6 +50,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     if (part > 0 && part * int64_t(keys) >= s.kv) return;
     const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
     const float c2 = a.scale * kLog2e;
+    const int shift = __builtin_ctz(c.page);
 
     for (int tile = k % plan.tiles; tile * int64_t(16 * NC) < rows; tile += plan.tiles) {
         typename M::QTile q[NC];
@@ -85,11 +88,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             typename M::VTile v;
             int kp, vp;
         };
-        auto load = [&](Stage& st, int t0, int kp, int vp) {
-            M::load_k(c, st.k, kp, hk, t0, lane);
-            M::load_v(c, st.v, vp, hk, t0, lane);
-            st.kp = kp;
-            st.vp = vp;
+        auto load = [&](Stage& st, int t0, int p0) {
+            st.kp = page_list[((t0 + M::k_group(lane)) >> shift) - p0];
+            st.vp = page_list[((t0 + M::v_group(lane)) >> shift) - p0];
+            M::load_k(c, st.k, st.kp, hk, t0, lane);
+            M::load_v(c, st.v, st.vp, hk, t0, lane);
         };
         auto compute = [&](Stage& st, int t0) {
             const bool masked =
@@ -138,21 +141,24 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             M::template output<NC>(st.v, pr, acc);
         };
 
-        // Two tiles in flight: one is computed while the next is loaded, and the page
-        // numbers of the one after that are on their way. (With 32 rows the registers hold
-        // one tile; the CU's other waves cover its loads.)
+        // Two tiles in flight: one is computed while the next is loaded. (With 32 rows the
+        // registers hold one tile; the CU's other waves cover its loads.) The page numbers of
+        // the next 16,384 keys lie in LDS: a load of them would return in order with the rows
+        // asked for before.
         constexpr int JUMP = 4 * KEYS;
-        int t0 = lo + wave * KEYS;
-        if (t0 < end) {
+        for (int seg = lo; seg < end; seg += kSegment) {
+            const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
+            const int entries = ((((seg_end + JUMP - 1) & -JUMP) - 1) >> shift) - p0 + 1;
+            __syncthreads();  // the list before has been read
+            for (int e = threadIdx.x; e < entries; e += 256)
+                page_list[e] = page_of(c.table, c.width, c.pages, b, p0 + e);
+            __syncthreads();
+            int t0 = seg + wave * KEYS;
+            if (t0 >= seg_end) continue;
             Stage A;
-            load(A, t0, M::k_page(c, b, t0, lane), M::v_page(c, b, t0, lane));
-            int kp = M::k_page(c, b, t0 + JUMP, lane), vp = M::v_page(c, b, t0 + JUMP, lane);
+            load(A, t0, p0);
             auto next = [&](Stage& st) {
-                if (t0 + JUMP < end) {
-                    load(st, t0 + JUMP, kp, vp);
-                    kp = M::k_page(c, b, t0 + 2 * JUMP, lane);
-                    vp = M::v_page(c, b, t0 + 2 * JUMP, lane);
-                }
+                if (t0 + JUMP < seg_end) load(st, t0 + JUMP, p0);
             };
             if constexpr (NC == 1) {
                 Stage B;
@@ -160,18 +166,18 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
                     next(B);
                     compute(A, t0);
                     t0 += JUMP;
-                    if (t0 >= end) break;
+                    if (t0 >= seg_end) break;
                     next(A);
                     compute(B, t0);
                     t0 += JUMP;
-                    if (t0 >= end) break;
+                    if (t0 >= seg_end) break;
                 }
             } else {
                 for (;;) {
                     compute(A, t0);
                     next(A);
                     t0 += JUMP;
-                    if (t0 >= end) break;
+                    if (t0 >= seg_end) break;
                 }
             }
         }
@@ -289,9 +295,15 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 
 // The launch for what is known of the lengths. bf16 rows of more than 32 a sequence go to
 // the kernel of 128-row tiles; others are taken 16 at a time, or 32 where there are more than
-// 16. The keys are split until there are four workgroups per CU, but into parts of at
-// least 512 keys (a part's prologue and merge cost as much as about a hundred keys), and no
-// more than the workspace holds.
+// 16. The keys are split until there are sixteen workgroups per CU, not for the number of them
+// (two fill a CU) but so that a ragged batch fills the GPU to the end: 64 sequences of 400 to
+// 9,001 tokens take 195 us whole, 155, 150, 142 and 146 us in 2, 4, 8 and 16 parts (64 of 2,560
+// each take 118 us whole and 131 us in 5 parts). A part is at least four rounds of the
+// workgroup's waves, and a cache of up to eight rounds stays whole: the second kernel costs
+// what four rounds cost (613 float32 tokens: 13.8 us whole, 16.4 us in 2 parts). Tiles of 128
+// rows see keys of like numbers and are split to fill the GPU only (chunks of 1,531 and 2,048
+// tokens, 896 workgroups: 2.12 ms whole, 2.27 ms in 2 parts). There are no more parts than
+// the workspace holds.
 struct Shape {
     PagedPlan plan;
     int rows;       // of a tile
@@ -311,13 +323,15 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int64_t pairs = int64_t(c.B) * c.H;
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
     tiles = std::min(tiles, room);
-    int64_t parts = std::min<int64_t>((most_kv + 511) / 512,
-                                      4 * kCus / std::min<int64_t>(pairs * tiles, 4 * kCus));
+    const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
+    int64_t parts = most_kv <= 8 * round ? 1 : (most_kv + 4 * round - 1) / (4 * round);
+    const int64_t wanted = (r.rows == 128 ? 4 : 16) * kCus;
+    parts = std::min<int64_t>(parts, wanted / std::min<int64_t>(pairs * tiles, wanted));
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);
-    r.plan.step = std::max(512, int(((most_kv + parts - 1) / parts + 127) / 128 * 128));
+    r.plan.step = std::max(4 * round, int(((most_kv + parts - 1) / parts + 127) / 128 * 128));
     r.bytes = parts > 1 ? parts * part_bytes : 0;
     return r;
 }

@@ -110,7 +110,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int turn = blockIdx.x >> 3;
     const int unit = turn / plan.tiles * 8 + (blockIdx.x & 7);
     if (unit >= units) return;
-    const int part = unit % plan.parts, bh = unit / plan.parts;
+    const auto [bh, part] = unit_of(unit, c.B * c.H);
     const int b = bh / c.H, hk = bh % c.H;
     const int G = a.q_heads / c.H;
     const Seq s = sequence(c, a.tokens, b);

@@ -68,12 +68,6 @@ struct TileMath<uint16_t, D> {
     static __device__ __forceinline__ int key_of(int g, int v) { return 8 * g + v; }
     static __device__ __forceinline__ int k_group(int lane) { return 8 * ((lane & 15) >> 2); }
     static __device__ __forceinline__ int v_group(int lane) { return 8 * (lane >> 4); }
-    static __device__ __forceinline__ int k_page(const sparsp_cache& c, int b, int t0, int lane) {
-        return page_of(c.table, c.width, c.pages, b, (t0 + k_group(lane)) >> __builtin_ctz(c.page));
-    }
-    static __device__ __forceinline__ int v_page(const sparsp_cache& c, int b, int t0, int lane) {
-        return page_of(c.table, c.width, c.pages, b, (t0 + v_group(lane)) >> __builtin_ctz(c.page));
-    }
 
     static __device__ __forceinline__ void load_k(const sparsp_cache& c, KTile& t, int page, int hk,
                                                   int t0, int lane) {
@@ -171,13 +165,8 @@ struct TileMath<float, D> {
     struct VTile { float r[4][DV]; };
 
     static __device__ __forceinline__ int key_of(int g, int v) { return 4 * g + v; }
+    static __device__ __forceinline__ int k_group(int) { return 0; }
     static __device__ __forceinline__ int v_group(int lane) { return 4 * (lane >> 4); }
-    static __device__ __forceinline__ int k_page(const sparsp_cache& c, int b, int t0, int) {
-        return page_of(c.table, c.width, c.pages, b, t0 >> __builtin_ctz(c.page));
-    }
-    static __device__ __forceinline__ int v_page(const sparsp_cache& c, int b, int t0, int) {
-        return page_of(c.table, c.width, c.pages, b, t0 >> __builtin_ctz(c.page));
-    }
 
     static __device__ __forceinline__ void load_k(const sparsp_cache& c, KTile& t, int page, int hk,
                                                   int t0, int lane) {

@@ -25,7 +25,8 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(const PagedArgs a, i
     constexpr int KEYS = M::KEYS;
     for (int t0 = (first * 4 + wave) * KEYS; t0 < s.kv; t0 += strides * 4 * KEYS) {
         typename M::KTile k;
-        const int page = M::k_page(c, b, t0, lane);
+        const int page = page_of(c.table, c.width, c.pages, b,
+                                 (t0 + M::k_group(lane)) >> __builtin_ctz(c.page));
         M::load_k(c, k, page, hk, t0, lane);
         float w[M::PER] = {};
         // Rows before r_first see none of these keys.

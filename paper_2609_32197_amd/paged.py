@@ -22,8 +22,7 @@ import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
-from . import (_SIGNATURES, _RESTYPES, _check, _empty, _stream, _torch, BF16, F32, SparspError,
-               load_library)
+from . import _SIGNATURES, _RESTYPES, _check, _empty, _torch, BF16, F32, load_library
 
 __all__ = [
     "Rotary",
@@ -105,39 +104,46 @@ def _dtype_code(t, name):
     raise ValueError(f"{name} must be bfloat16 or float32 (got {t.dtype})")
 
 
-def _on(t, name, device, dtype=None, shape=None):
-    """Address of a contiguous tensor on `device` (None: any GPU)."""
-    if not isinstance(t, _torch().Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on the GPU (got {t.device})")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} must be on {device} (got {t.device})")
+# (Host time is what the smallest calls are bound by. get_device() is the device's index, -1
+# off the GPU, at a fraction of what comparing device objects costs.)
+def _on(t, name, index, dtype=None, shape=None):
+    """Address of a contiguous tensor on GPU `index` (None: any)."""
+    try:
+        at = t.get_device()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    if at < 0 or (at != index and index is not None):
+        raise ValueError(f"{name} must be on the GPU" + (
+            "" if index is None else f" cuda:{index}") + f" (got {t.device})")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
     return t.data_ptr()
 
 
-def _rows(t, name, device, dtype, tokens, d, heads=None):
+def _rows(t, name, index, dtype, tokens, d, heads=None):
     """sparsp_rows of a [heads, tokens, d] tensor."""
-    if not isinstance(t, _torch().Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dim() != 3 or not t.is_cuda or t.device != device or t.dtype != dtype:
-        raise ValueError(f"{name} must be a [heads, tokens, d] {dtype} tensor on {device} (got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device})")
-    h, n, c = t.shape
+    try:
+        at, shape = t.get_device(), t.shape
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    if len(shape) != 3 or at != index or t.dtype is not dtype:
+        raise ValueError(f"{name} must be a [heads, tokens, d] {dtype} tensor on the GPU "
+                         f"cuda:{index} (got {tuple(shape)} {t.dtype} on {t.device})")
+    h, n, c = shape
     if n != tokens or c != d or (heads is not None and h != heads):
-        raise ValueError(f"{name} must have shape {(heads or h, tokens, d)} (got {tuple(t.shape)})")
+        raise ValueError(f"{name} must have shape {(heads or h, tokens, d)} (got {tuple(shape)})")
     sh, st, sc = t.stride()
     if sc != 1:
         raise ValueError(f"{name} must have contiguous channels")
     # An axis of one entry, or a tensor of none, is never stepped along.
-    if n <= 1 or h <= 1 or not n:
-        sh, st = (sh if h > 1 else d), (st if n > 1 else d)
+    if n <= 1:
+        st = d
+    if h <= 1 or not n:
+        sh = d
     return _ROWS.pack(t.data_ptr() or 16, sh, st, h, 0)
 
 
@@ -150,32 +156,34 @@ def _like_rows(x, dtype=None):
     return torch.empty((h, n, d), dtype=dtype or x.dtype, device=x.device)
 
 
-class _On:
-    """The library call with `device` current, which launches need."""
+def _call(fn, index, stream, *args):
+    """The library call on GPU `index`, which launches need to be current, and its stream."""
+    cuda = _torch()._C
+    if stream is None:
+        raw = cuda._cuda_getCurrentRawStream(index)
+    elif stream.device.index != index:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+    else:
+        raw = stream.cuda_stream
+    if cuda._cuda_getDevice() == index:
+        rc = fn(*args, raw)
+    else:
+        with _torch().cuda.device(index):
+            rc = fn(*args, raw)
+    if rc < 0:
+        _check(rc)
 
-    def __init__(self, device, stream):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        self.device, self.stream = device, _stream(stream, device)
 
-    def call(self, fn, *args):
-        torch = _torch()
-        if torch._C._cuda_getDevice() == self.device.index:
-            return _check(fn(*args, self.stream))
-        with torch.cuda.device(self.device):
-            return _check(fn(*args, self.stream))
-
-
-def _positions(rotary, positions, inv_freq, tokens, device):
+def _positions(rotary, positions, inv_freq, tokens, index):
     torch = _torch()
     if not isinstance(positions, torch.Tensor):
         raise TypeError("positions must be a torch.Tensor")
     if positions.dtype not in (torch.int32, torch.int64):
         raise ValueError(f"positions must be int32 or int64 (got {positions.dtype})")
     p = positions if positions.dim() == 2 else positions.view(1, -1)
-    return (_on(p, "positions", device, None, (rotary.axes, tokens)) or 16,
+    return (_on(p, "positions", index, None, (rotary.axes, tokens)) or 16,
             32 if positions.dtype == torch.int32 else 64,
-            _on(inv_freq, "inv_freq", device, torch.float32, (rotary.rot_dim // 2,)))
+            _on(inv_freq, "inv_freq", index, torch.float32, (rotary.rot_dim // 2,)))
 
 
 def sparsp_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "plain",
@@ -212,8 +220,7 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     code = _dtype_code(X, "X")
     if X.dim() != 3 or not X.is_cuda:
         raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
-    dev, (_, n, d) = X.device, X.shape
-    on = _On(dev, stream)
+    dev, (_, n, d) = X.get_device(), X.shape
     y = Y if Y is not None else _like_rows(X)
     x, o, count = _rows(X, "X", dev, X.dtype, n, d), _rows(y, "Y", dev, X.dtype, n, d, X.shape[0]), 1
     y2 = None
@@ -225,23 +232,24 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     elif Y2 is not None:
         raise ValueError("Y2 needs X2")
     pos, bits, freq = _positions(rotary, positions, inv_freq, n, dev)
-    on.call(load_library().sparsp_rope, rotary._pack(inverse), n, d, code, x, o, count, pos, bits,
+    _call(load_library().sparsp_rope, dev, stream, rotary._pack(inverse), n, d, code, x, o, count, pos, bits,
             freq)
     return y if X2 is None else (y, y2)
 
 
 def _cache(K_cache, V_cache, weights, page_table, new_off, kv_len):
-    """(sparsp_cache, device) of the cache's tensors; V_cache, weights, new_off may be None."""
+    """(sparsp_cache, GPU) of the cache's tensors; V_cache, weights, new_off may be None."""
     torch = _torch()
     if not isinstance(K_cache, torch.Tensor):
         raise TypeError("K_cache must be a torch.Tensor")
     if K_cache.dim() != 4:
         raise ValueError("K_cache must be [pages, H, page, d]")
-    dev, shape, i32 = K_cache.device, K_cache.shape, torch.int32
+    shape, i32 = K_cache.shape, torch.int32
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be an int32 [B, width] tensor")
     B, width = page_table.shape
     k = _on(K_cache, "K_cache", None)
+    dev = K_cache.get_device()
     v = 0 if V_cache is None else _on(V_cache, "V_cache", dev, K_cache.dtype, shape)
     w = 0 if weights is None else _on(weights, "weights", dev, torch.float32, shape[:3])
     return _CACHE.pack(
@@ -260,7 +268,6 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
     be Q). Returns Q_out, or None without Q.
     """
     c, dev = _cache(K_cache, V_cache, weights, page_table, new_off, kv_len)
-    on = _On(dev, stream)
     if K.dim() != 3:
         raise ValueError("K must be [H, tokens, d]")
     H, n, d, dt = K_cache.shape[1], K.shape[1], K_cache.shape[3], K_cache.dtype
@@ -275,7 +282,7 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
         qo = _rows(Q_out, "Q_out", dev, dt, n, d, Q.shape[0])
     elif Q_out is not None:
         raise ValueError("Q_out needs Q")
-    on.call(load_library().sparsp_paged_append, c, n, _rows(K, "K", dev, dt, n, d, H),
+    _call(load_library().sparsp_paged_append, dev, stream, c, n, _rows(K, "K", dev, dt, n, d, H),
             _rows(V, "V", dev, dt, n, d, H), rot, pos, bits, freq, q, qo)
     return Q_out
 
@@ -309,7 +316,6 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, None, page_table, new_off, kv_len)
-    on = _On(dev, stream)
     d, dt = K_cache.shape[3], K_cache.dtype
     if Q.dim() != 3:
         raise ValueError("Q must be [heads, tokens, d]")
@@ -323,7 +329,7 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     if workspace is not None:
         ws = _on(workspace, "workspace", dev)
         nbytes = workspace.numel() * workspace.element_size()
-    on.call(load_library().sparsp_paged_attn, c, n, _rows(Q, "Q", dev, dt, n, d),
+    _call(load_library().sparsp_paged_attn, dev, stream, c, n, _rows(Q, "Q", dev, dt, n, d),
             _rows(o, "O", dev, odt, n, d, heads), int(out_dtype),
             None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
             bool(causal), _scale(softmax_scale, d), int(max_new or 0), int(max_kv or 0), ws, nbytes)
@@ -341,7 +347,6 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
     """
     torch = _torch()
     c, dev = _cache(K_cache, None, weights, page_table, new_off, kv_len)
-    on = _On(dev, stream)
     if Q.dim() != 3:
         raise ValueError("Q must be [heads, tokens, d]")
     heads, n, d = Q.shape
@@ -349,7 +354,7 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
         raise ValueError(f"Q must have d = {K_cache.shape[3]} (got {d})")
     if weights is None:
         raise TypeError("weights must be a torch.Tensor")
-    on.call(load_library().sparsp_paged_weights, c, n, _rows(Q, "Q", dev, K_cache.dtype, n, d),
+    _call(load_library().sparsp_paged_weights, dev, stream, c, n, _rows(Q, "Q", dev, K_cache.dtype, n, d),
             _on(lse, "lse", dev, torch.float32, (heads, n)) or 16, bool(causal),
             _scale(softmax_scale, d), bool(accumulate), int(max_new or 0), int(max_kv or 0))
     return weights
@@ -365,7 +370,6 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
-    on = _On(dev, stream)
     B, H, keep = page_table.shape[0], K_cache.shape[1], int(keep)
     out = kv_len_out if kv_len_out is not None else torch.empty_like(kv_len)
     lst = kept if kept is not None else _empty((B, H, max(keep, 0)), torch.int32, K_cache)
@@ -374,7 +378,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
         if dst_table.dim() != 2 or dst_table.shape[0] != B:
             raise ValueError(f"dst_table must be an int32 [{B}, width] tensor")
         dst, dst_width = _on(dst_table, "dst_table", dev, torch.int32), dst_table.shape[1]
-    on.call(load_library().sparsp_cache_evict, c, keep, int(first), int(recent), dst, dst_width,
+    _call(load_library().sparsp_cache_evict, dev, stream, c, keep, int(first), int(recent), dst, dst_width,
             _on(out, "kv_len_out", dev, torch.int32, (B,)),
             _on(lst, "kept", dev, torch.int32, (B, H, max(keep, 0))))
     return out, lst
