@@ -200,10 +200,18 @@ int sparsp_paged_weights(const sparsp_cache* cache, int32_t tokens, const sparsp
  * which may be a page of `table`, and the old pages stay as they were. Pages must not be
  * shared between sequences (or heads would move twice). A token on a bad page weighs as NaN and
  * moves nothing. first + recent <= keep; keep >= 1.
+ *
+ * workspace: 16-byte aligned device memory or NULL, contents irrelevant, not shared by calls that
+ * overlap. With sparsp_cache_evict_workspace_bytes bytes the choice in few long sequences is
+ * shared out over more workgroups; the result is the same.
  */
 int sparsp_cache_evict(const sparsp_cache* cache, int32_t keep, int32_t first, int32_t recent,
                        const int32_t* dst_table, int32_t dst_width, int32_t* kv_len_out,
-                       int32_t* kept, void* stream);
+                       int32_t* kept, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes that sparsp_cache_evict can use for this cache's shape (0: none), or a negative
+ * status. Host only; the cache's pointers are not read. */
+int64_t sparsp_cache_evict_workspace_bytes(const sparsp_cache* cache);
 
 #ifdef __cplusplus
 }

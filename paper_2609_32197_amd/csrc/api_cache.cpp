@@ -332,9 +332,15 @@ int sparsp_paged_weights(const sparsp_cache* cache, int32_t tokens, const sparsp
     return hip_status(sparsp::launch_paged_weights(a, (hipStream_t)stream), "sparsp_paged_weights");
 }
 
+int64_t sparsp_cache_evict_workspace_bytes(const sparsp_cache* cache) {
+    if (int rc = check_cache(cache)) return rc;
+    ok();
+    return sparsp::evict_workspace(*cache);
+}
+
 int sparsp_cache_evict(const sparsp_cache* cache, int32_t keep, int32_t first, int32_t recent,
                        const int32_t* dst_table, int32_t dst_width, int32_t* kv_len_out,
-                       int32_t* kept, void* stream) {
+                       int32_t* kept, void* workspace, int64_t workspace_bytes, void* stream) {
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_pointers(cache, true, true, false)) return rc;
     if (!kv_len_out || !kept) return fail(SPARSP_E_INVALID, "kv_len_out or kept is NULL");
@@ -352,8 +358,12 @@ int sparsp_cache_evict(const sparsp_cache* cache, int32_t keep, int32_t first, i
             return fail(SPARSP_E_CAPACITY, "dst_width = %d pages of %d hold fewer than keep = %d",
                         dst_width, cache->page, keep);
     }
+    if (workspace_bytes < 0) return fail(SPARSP_E_INVALID, "workspace_bytes < 0");
+    if (!aligned16(workspace)) return fail(SPARSP_E_INVALID, "workspace must be 16-byte aligned");
     return hip_status(sparsp::launch_cache_evict(*cache, keep, first, recent, dst_table, dst_width,
-                                                 kv_len_out, kept, (hipStream_t)stream),
+                                                 kv_len_out, kept, workspace,
+                                                 workspace ? workspace_bytes : 0,
+                                                 (hipStream_t)stream),
                       "sparsp_cache_evict");
 }
 

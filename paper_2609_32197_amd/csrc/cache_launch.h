@@ -66,6 +66,8 @@ hipError_t launch_paged_weights(const PagedArgs& a, hipStream_t s);
 
 hipError_t launch_cache_evict(const sparsp_cache& c, int keep, int first, int recent,
                               const int32_t* dst_table, int dst_width, int32_t* kv_len_out,
-                              int32_t* kept, hipStream_t s);
+                              int32_t* kept, void* ws, int64_t ws_bytes, hipStream_t s);
+// Bytes of workspace that its choice can use.
+int64_t evict_workspace(const sparsp_cache& c);
 
 }  // namespace sparsp

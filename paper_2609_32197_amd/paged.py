@@ -33,6 +33,7 @@ __all__ = [
     "sparsp_paged_attn_workspace_bytes",
     "sparsp_paged_weights",
     "sparsp_cache_evict",
+    "sparsp_cache_evict_workspace_bytes",
     "rope_frequencies",
     "rope",
     "paged_append",
@@ -40,6 +41,7 @@ __all__ = [
     "paged_attn_workspace_bytes",
     "paged_weights",
     "cache_evict",
+    "cache_evict_workspace_bytes",
 ]
 
 _VP, _I32, _I64, _F32, _F64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
@@ -59,9 +61,11 @@ _SIGNATURES.update({
                           _I64, _VP],
     "sparsp_paged_attn_workspace_bytes": [_STRUCT, _I32, _I32, _I32, _I32],
     "sparsp_paged_weights": [_STRUCT, _I32, _STRUCT, _VP, _I32, _F32, _I32, _I32, _I32, _VP],
-    "sparsp_cache_evict": [_STRUCT, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP],
+    "sparsp_cache_evict": [_STRUCT, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I64, _VP],
+    "sparsp_cache_evict_workspace_bytes": [_STRUCT],
 })
 _RESTYPES["sparsp_paged_attn_workspace_bytes"] = _I64
+_RESTYPES["sparsp_cache_evict_workspace_bytes"] = _I64
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
@@ -361,12 +365,15 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
 
 
 def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int, first: int = 0,
-                       recent: int = 0, dst_table=None, kv_len_out=None, kept=None, stream=None):
+                       recent: int = 0, dst_table=None, kv_len_out=None, kept=None, workspace=None,
+                       stream=None):
     """Cuts every sequence of more than `keep` tokens to `keep`: its first and recent ones, and
     of the others, per head, those of most weight. Returns (kv_len_out [B], kept [B, H, keep]).
 
     The kept tokens move to the front of the sequence's pages, or into the pages of dst_table
-    (int32 [B, width], none of them in page_table). kept lists them, ascending, then -1.
+    (int32 [B, width], none of them in page_table). kept lists them, ascending, then -1. Few long
+    sequences use a workspace (sparsp_cache_evict_workspace_bytes bytes), which is allocated here
+    unless one is given, like the outputs.
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
@@ -378,10 +385,29 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
         if dst_table.dim() != 2 or dst_table.shape[0] != B:
             raise ValueError(f"dst_table must be an int32 [{B}, width] tensor")
         dst, dst_width = _on(dst_table, "dst_table", dev, torch.int32), dst_table.shape[1]
-    _call(load_library().sparsp_cache_evict, dev, stream, c, keep, int(first), int(recent), dst, dst_width,
-            _on(out, "kv_len_out", dev, torch.int32, (B,)),
-            _on(lst, "kept", dev, torch.int32, (B, H, max(keep, 0))))
+    lib = load_library()
+    if workspace is None:
+        nbytes = lib.sparsp_cache_evict_workspace_bytes(c)
+        if nbytes > 0:
+            workspace = _empty((nbytes,), torch.uint8, K_cache)
+            if stream is not None:
+                workspace.record_stream(stream)
+    ws = None if workspace is None else _on(workspace, "workspace", dev)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call(lib.sparsp_cache_evict, dev, stream, c, keep, int(first), int(recent), dst, dst_width,
+          _on(out, "kv_len_out", dev, torch.int32, (B,)),
+          _on(lst, "kept", dev, torch.int32, (B, H, max(keep, 0))), ws, nbytes)
     return out, lst
+
+
+def sparsp_cache_evict_workspace_bytes(K_cache, page_table) -> int:
+    """Workspace bytes that sparsp_cache_evict can use for these shapes (host)."""
+    B, width = page_table.shape
+    P, H, page, d = K_cache.shape
+    c = _CACHE.pack(0, 0, 0, 0, 0, 0, P, H, page, d, _dtype_code(K_cache, "K_cache"), width, B, 0)
+    n = int(load_library().sparsp_cache_evict_workspace_bytes(c))
+    _check(n if n < 0 else 0)
+    return n
 
 
 rope_frequencies = sparsp_rope_frequencies
@@ -391,3 +417,4 @@ paged_attn = sparsp_paged_attn
 paged_attn_workspace_bytes = sparsp_paged_attn_workspace_bytes
 paged_weights = sparsp_paged_weights
 cache_evict = sparsp_cache_evict
+cache_evict_workspace_bytes = sparsp_cache_evict_workspace_bytes

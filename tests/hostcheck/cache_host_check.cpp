@@ -73,7 +73,8 @@ struct Call {
         return sparsp_paged_weights(&c, tokens, &Q, lse, 1, scale, 1, max_new, max_kv, nullptr);
     }
     int evict() {
-        return sparsp_cache_evict(&c, keep, first, recent, dst, dst_width, len, kept, nullptr);
+        return sparsp_cache_evict(&c, keep, first, recent, dst, dst_width, len, kept, ws, ws_bytes,
+                                  nullptr);
     }
     int rope() { return sparsp_rope(&r, tokens, 64, c.dtype, &Q, &O, 1, pos, bits, freq, nullptr); }
 };
@@ -139,8 +140,8 @@ int main() {
         {"scale inf", ATTEND | WEIGH, I, [](Call& x) { x.scale = INFINITY; }},
         {"max_new < 0", ATTEND | WEIGH, I, [](Call& x) { x.max_new = -1; }},
         {"max_kv < 0", ATTEND | WEIGH, I, [](Call& x) { x.max_kv = -1; }},
-        {"workspace misaligned", ATTEND, I, [](Call& x) { x.ws = at((11 << 20) + 4); }},
-        {"workspace_bytes < 0", ATTEND, I, [](Call& x) { x.ws_bytes = -1; }},
+        {"workspace misaligned", ATTEND | EVICT, I, [](Call& x) { x.ws = at((11 << 20) + 4); }},
+        {"workspace_bytes < 0", ATTEND | EVICT, I, [](Call& x) { x.ws_bytes = -1; }},
         {"lse NULL", WEIGH, I, [](Call& x) { x.lse = nullptr; }},
         {"rot_dim odd", APPEND | ROPE, I, [](Call& x) { x.r.rot_dim = 33; }},
         {"rot_dim 0", APPEND | ROPE, I, [](Call& x) { x.r.rot_dim = 0; }},
@@ -181,7 +182,7 @@ int main() {
     }
     Call x;
     expect("cache NULL", sparsp_paged_attn(nullptr, 5, &x.Q, &x.O, 1, nullptr, 1, 1.f, 0, 0, nullptr, 0, nullptr), I, 0);
-    expect("cache NULL", sparsp_cache_evict(nullptr, 1, 0, 0, nullptr, 0, x.len, x.kept, nullptr), I, 0);
+    expect("cache NULL", sparsp_cache_evict(nullptr, 1, 0, 0, nullptr, 0, x.len, x.kept, nullptr, 0, nullptr), I, 0);
     expect("K alone", sparsp_paged_append(&x.c, 5, &x.K, &x.V, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr), SPARSP_OK, 1);
     expect("Q, no rotation", sparsp_paged_append(&x.c, 5, &x.K, &x.V, nullptr, nullptr, 0, nullptr, &x.Q, &x.O, nullptr), I, 0);
     expect("Q, no Q_out", sparsp_paged_append(&x.c, 5, &x.K, &x.V, &x.r, x.pos, 32, x.freq, &x.Q, nullptr, nullptr), I, 0);
@@ -197,6 +198,9 @@ int main() {
     expect("workspace of none", sparsp_paged_attn_workspace_bytes(&x.c, 0, 4, 0, 0), 0, 0);
     expect("workspace heads", sparsp_paged_attn_workspace_bytes(&x.c, 5, 3, 0, 0), I, 0);
     expect("workspace NULL", sparsp_paged_attn_workspace_bytes(nullptr, 5, 4, 0, 0), I, 0);
+
+    expect("evict workspace", sparsp_cache_evict_workspace_bytes(&x.c), 8192, 0);
+    expect("evict workspace NULL", sparsp_cache_evict_workspace_bytes(nullptr), I, 0);
 
     float f[128], s;
     expect("frequencies", sparsp_rope_frequencies(256, 1e4, 0, 0, 0, 0, 0, f, &s), SPARSP_OK, 0);

@@ -15,6 +15,7 @@ hipError_t launch_paged_attn(const PagedArgs&, hipStream_t) { return launched();
 int64_t paged_attn_workspace(const PagedArgs&) { return 4096; }
 hipError_t launch_paged_weights(const PagedArgs&, hipStream_t) { return launched(); }
 hipError_t launch_cache_evict(const sparsp_cache&, int, int, int, const int32_t*, int, int32_t*,
-                              int32_t*, hipStream_t) { return launched(); }
+                              int32_t*, void*, int64_t, hipStream_t) { return launched(); }
+int64_t evict_workspace(const sparsp_cache&) { return 8192; }
 
 }  // namespace sparsp

@@ -40,7 +40,7 @@ def test_abi_under_asan_and_ubsan(tmp_path):
 def test_library_exports_every_declared_symbol():
     text = open(os.path.join(ROOT, "include", "sparsp_cache.h")).read()
     names = re.findall(r"^(?:int|int64_t)\s+(sparsp_\w+)\s*\(", text, re.M)
-    assert len(names) == 7
+    assert len(names) == 8
     for name in names:
         assert hasattr(sp.load_library(), name), name
 
@@ -106,3 +106,7 @@ def test_workspace_bytes():
     assert n > 0 and n % (2 * 4 * 65 * 4) == 0
     with pytest.raises(sp.SparspError):
         sp.sparsp_paged_attn_workspace_bytes(c, t, 2, 3)
+    assert sp.sparsp_cache_evict_workspace_bytes(c, t) == 0  # 4,800 tokens: one workgroup each
+    long = torch.zeros(2, 3000, dtype=torch.int32)
+    n = sp.sparsp_cache_evict_workspace_bytes(c, long)
+    assert n >= 4 * 2 * 2 * 48000 and n % 16 == 0

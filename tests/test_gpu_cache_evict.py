@@ -103,28 +103,48 @@ def test_weights_that_tie_or_are_not_numbers(gpu, kind):
         check(bt, keep, first, recent)
 
 
-def test_one_long_cache(gpu):
-    """A choice among many tokens, whose keys share their leading digits."""
-    n, keep = 70001, 9999
-    H, d, page = 2, 16, 64
-    pages = -(-n // page)
+@pytest.mark.parametrize("n,keep,first,recent,page,kind", [
+    (70001, 9999, 7, 50, 64, "close"),
+    (70001, 66000, 0, 0, 16, "spread"),
+    (40000, 39999, 64, 65, 256, "equal"),     # every key at the first digit
+    (33001, 1, 0, 0, 32, "spread"),
+    (66000, 30000, 20000, 10000, 64, "spread"),  # nothing to choose
+])
+@pytest.mark.parametrize("space", ["given", "own", "small"])
+def test_long_caches(gpu, n, keep, first, recent, page, kind, space):
+    """A choice among many tokens, shared out over workgroups (or, with too small a
+    workspace, not); "close": keys that share their leading digits. Beside a short one."""
+    H, d, B = 2, 8, 2
+    width = -(-n // page) + 3
+    pages = B * width
     g = torch.Generator().manual_seed(2)
-    table = torch.randperm(pages, generator=g).to(torch.int32).view(1, -1)
-    w = 1.0 + torch.randint(0, 3000, (pages, H, page), generator=g).float() * 2.0 ** -23
+    table = torch.randperm(pages, generator=g).to(torch.int32).view(B, width)
+    w = torch.randint(0, 3000, (pages, H, page), generator=g).float()
+    w = {"close": 1.0 + w * 2.0 ** -23, "spread": torch.exp(w / 200 - 9),
+         "equal": torch.full_like(w, 0.5)}[kind]
     K = torch.randn(pages, H, page, d, generator=g).to(BF)
     k, v, ww = K.cuda(), (-K).cuda(), w.cuda()
-    kv = torch.tensor([n], dtype=torch.int32, device="cuda")
-    out, kept = sp.sparsp_cache_evict(k, v, ww, table.cuda(), kv, keep, 7, 50)
+    lens = (n, min(keep, 5))
+    kv = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    need = sp.sparsp_cache_evict_workspace_bytes(k, table)
+    assert need > 0
+    ws = None if space == "own" else torch.full((need - 16 * (space == "small"),), 255,
+                                                dtype=torch.uint8, device="cuda")
+    out, kept = sp.sparsp_cache_evict(k, v, ww, table.cuda(), kv, keep, first, recent, workspace=ws)
+    assert out.tolist() == [min(x, keep) for x in lens]
+    kk, vv, w2 = k.cpu(), v.cpu(), ww.cpu()
     t = torch.arange(n)
     p, r = table[0].long()[t // page], t % page
     j = torch.arange(keep)
     q, s = table[0].long()[j // page], j % page
     for h in range(H):
         x = w[p, h, r].clone()
-        x[:7] = x[n - 50:] = float("inf")
+        x[:first] = x[n - recent:] = float("inf")
         stay = torch.sort(torch.sort(-x, stable=True).indices[:keep]).values
         assert torch.equal(kept[0, h].cpu().long(), stay)
-        assert torch.equal(k.cpu()[q, h, s], K[p, h, r][stay])
-        assert torch.equal(v.cpu()[q, h, s], -K[p, h, r][stay])
-        assert torch.equal(ww.cpu()[q, h, s], w[p, h, r][stay])
-    assert out.item() == keep
+        assert torch.equal(kk[q, h, s], K[p, h, r][stay])
+        assert torch.equal(vv[q, h, s], -K[p, h, r][stay])
+        assert torch.equal(w2[q, h, s], w[p, h, r][stay])
+        assert kept[1, h].tolist() == list(range(lens[1])) + [-1] * (keep - lens[1])
+    p1 = table[1].long()
+    assert torch.equal(kk[p1], K[p1]) and torch.equal(w2[p1], w[p1])
