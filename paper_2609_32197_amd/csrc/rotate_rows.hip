@@ -27,11 +27,13 @@ struct Move {
     int64_t dst_head, dst_token;
     Div heads, units;
     int paged, rotate;
+    int tokens_first;  // a head's rows lie token after token
 };
 
 struct Params {
     Move move[3];
-    int moves, tokens, per, d, P, layout, inverse, wide;
+    int moves, tokens, d, P, layout, inverse, wide, stream;
+    Div per;  // tokens of a workgroup
     int axis_end[3];
     float factor;
     const void* positions;
@@ -56,40 +58,45 @@ template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {
     T e[V];
 };
+// Rows that no cache can hold until they are read again leave none of themselves in one.
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> get(const Vec<T, V>* p, bool stream) {
+    if constexpr (sizeof(T) * V == 16)
+        if (stream)
+            return __builtin_bit_cast(Vec<T, V>, load_nt(reinterpret_cast<const char*>(p)));
+    return *p;
+}
+template <typename T, int V>
+__device__ __forceinline__ void put(Vec<T, V>* p, Vec<T, V> x, bool stream) {
+    if constexpr (sizeof(T) * V == 16)
+        if (stream) return store_nt(reinterpret_cast<char*>(p), __builtin_bit_cast(uint4, x));
+    *p = x;
+}
 
-// A workgroup's places: for each token the byte offset of its row in the pages, or -1.
-// new_off is ascending, so the sequence of token t is the number of ends new_off[1..B] at
-// or before t, counted by all threads at once.
+// A workgroup's places: for each token the byte offset of its row in the pages, or -1. A wave
+// takes a token: new_off is ascending, so the token's sequence is the number of ends
+// new_off[1..B] at or before it, counted 64 at a time.
 template <typename T>
-__device__ __forceinline__ void find_places(const Params& p, int t0, int count, int64_t* place,
-                                            int* ends) {
+__device__ __forceinline__ void find_places(const Params& p, int t0, int count, int64_t* place) {
     const sparsp_cache& c = p.cache;
-    for (int k = 0; k < count; ++k) {
-        int mine = 0;
-        for (int b = threadIdx.x; b < c.B; b += kThreads) mine += c.new_off[b + 1] <= t0 + k;
-        for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
-        if ((threadIdx.x & 63) == 0) ends[k * (kThreads / 64) + (threadIdx.x >> 6)] = mine;
-    }
-    __syncthreads();
-    if (int(threadIdx.x) < count) {
-        const int k = threadIdx.x;
+    const int lane = threadIdx.x & 63;
+    for (int k = threadIdx.x >> 6; k < count; k += kThreads / 64) {
         int b = 0;
-        for (int w = 0; w < kThreads / 64; ++w) b += ends[k * (kThreads / 64) + w];
-        int64_t at = -1;
+        for (int e = lane; e < c.B; e += 64) b += c.new_off[e + 1] <= t0 + k;
+        for (int off = 32; off; off >>= 1) b += __shfl_xor(b, off);
+        int64_t row = -1;  // of head 0
         if (b < c.B) {
             const Seq s = sequence(c, p.tokens, b);
             const int i = t0 + k - s.q0, slot = s.kv - s.n + i;
             if (i >= 0 && i < s.n && slot >= 0) {
-                const int page = page_of(c.table, c.width, c.pages, b, slot / c.page);
-                if (page >= 0)
-                    at = (int64_t(page) * c.H * c.page + slot % c.page) * c.d;
+                const int shift = __builtin_ctz(c.page);
+                const int page = page_of(c.table, c.width, c.pages, b, slot >> shift);
+                if (page >= 0) row = int64_t(page) * c.H * c.page + (slot & (c.page - 1));
             }
         }
-        place[k] = at < 0 ? -1 : at * int64_t(sizeof(T));
-        if (at >= 0 && c.weights) {
-            const int64_t row = at / c.d;  // (page * H) * rows of a page + row of the page
-            for (int h = 0; h < c.H; ++h) c.weights[row + int64_t(h) * c.page] = 0.f;
-        }
+        if (lane == 0) place[k] = row < 0 ? -1 : row * c.d * int64_t(sizeof(T));
+        if (row >= 0 && c.weights)
+            for (int h = lane; h < c.H; h += 64) c.weights[row + int64_t(h) * c.page] = 0.f;
     }
 }
 
@@ -97,9 +104,8 @@ template <typename T, int V, bool HALF, bool PAGED>
 __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
     __shared__ float2 turn[kTableFloats];
     __shared__ int64_t place[kMaxPer];
-    __shared__ int ends[kMaxPer * (kThreads / 64)];
-    const int t0 = blockIdx.x * p.per, count = min(p.per, p.tokens - t0);
-    if (PAGED) find_places<T>(p, t0, count, place, ends);
+    const int t0 = blockIdx.x * p.per.d, count = min(int(p.per.d), p.tokens - t0);
+    if (PAGED) find_places<T>(p, t0, count, place);
     for (int e = threadIdx.x; e < count * p.P; e += kThreads) {
         const int k = e / p.P, pr = e % p.P;
         const int axis = (pr >= p.axis_end[0]) + (pr >= p.axis_end[1]);
@@ -114,14 +120,24 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
         turn[e] = make_float2(c * p.factor, (p.inverse ? -s : s) * p.factor);
     }
     __syncthreads();
+    const bool stream = p.stream;
 
     for (int m = 0; m < p.moves; ++m) {
         const Move& mv = p.move[m];
         const uint32_t heads = mv.heads.d, units = mv.units.d;
-        const uint32_t items = uint32_t(count) * heads * units;
+        // Rows are walked in the order in which they lie.
+        const uint32_t items = (mv.tokens_first ? p.per.d : uint32_t(count)) * heads * units;
         for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
             const uint32_t row = mv.units.quot(it), u = it - row * units;
-            const uint32_t k = mv.heads.quot(row), h = row - k * heads;
+            uint32_t k, h;
+            if (mv.tokens_first) {
+                h = p.per.quot(row);
+                k = row - h * p.per.d;
+                if (k >= uint32_t(count)) continue;
+            } else {
+                k = mv.heads.quot(row);
+                h = row - k * heads;
+            }
             const char* src = mv.src + int64_t(h) * mv.src_head + int64_t(t0 + k) * mv.src_token;
             char* dst = mv.dst;
             if (PAGED && mv.paged) {
@@ -136,12 +152,12 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
             const uint32_t turned = mv.rotate ? p.P * (HALF ? 1 : 2) / V : 0;  // units that rotate
             if (u >= turned) {
                 const uint32_t at = u + (HALF ? turned : 0);
-                out[at] = in[at];
+                put(out + at, get(in + at, stream), stream);
                 continue;
             }
             const float2* cs = turn + k * p.P;
             if (HALF) {
-                const Unit a = in[u], b = in[u + turned];
+                const Unit a = get(in + u, stream), b = get(in + u + turned, stream);
                 Unit ya, yb;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
@@ -150,10 +166,10 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
                     ya.e[e] = down<T>(x1 * t.x - x2 * t.y);
                     yb.e[e] = down<T>(x1 * t.y + x2 * t.x);
                 }
-                out[u] = ya;
-                out[u + turned] = yb;
+                put(out + u, ya, stream);
+                put(out + u + turned, yb, stream);
             } else if constexpr (V >= 2) {
-                const Unit a = in[u];
+                const Unit a = get(in + u, stream);
                 Unit y;
 #pragma unroll
                 for (int e = 0; e < V; e += 2) {
@@ -162,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
                     y.e[e] = down<T>(x1 * t.x - x2 * t.y);
                     y.e[e + 1] = down<T>(x1 * t.y + x2 * t.x);
                 }
-                out[u] = y;
+                put(out + u, y, stream);
             }
         }
     }
@@ -175,7 +191,7 @@ hipError_t launch_v(const RotateArgs& a, Params& p, bool paged, hipStream_t s) {
         const bool two = r.rotate && HALF;  // a rotating unit covers two accesses
         p.move[m].units = make_div(uint32_t(two ? (a.d - a.rot / 2) / V : a.d / V));
     }
-    const int grid = (a.tokens + p.per - 1) / p.per;
+    const int grid = (a.tokens + int(p.per.d) - 1) / int(p.per.d);
     if (paged)
         rotate_rows_kernel<T, V, HALF, true><<<grid, kThreads, 0, s>>>(p);
     else
@@ -202,7 +218,7 @@ hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
         p.move[m] = {static_cast<const char*>(r.src), r.src_head * size, r.src_token * size,
                      static_cast<char*>(r.dst),       r.dst_head * size, r.dst_token * size,
                      make_div(uint32_t(r.heads)),     make_div(1),       r.paged,
-                     r.rotate};
+                     r.rotate,                        r.src_token < r.src_head};
         paged |= r.paged;
         heads += r.heads;
     }
@@ -219,10 +235,12 @@ hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
     p.cache = a.cache;
     // Tokens of a workgroup: enough to fill the GPU four times with one each, more only
     // where there are so many that the angles are better shared by longer runs.
-    p.per = 1;
-    while (p.per < kMaxPer && a.tokens / (2 * p.per) >= 1024 &&
-           (p.P == 0 || 2 * p.per * p.P <= kTableFloats))
-        p.per *= 2;
+    int per = 1;
+    while (per < kMaxPer && a.tokens / (2 * per) >= 1024 &&
+           (p.P == 0 || 2 * per * p.P <= kTableFloats))
+        per *= 2;
+    p.per = make_div(uint32_t(per));
+    p.stream = int64_t(heads) * a.tokens * a.d * size > (int64_t(256) << 20);
     // The widest access that divides the rotated part (its half, where a unit is two
     // accesses) and the rest.
     const int part = a.rot == 0 ? a.d : a.layout == SPARSP_ROPE_HALF ? a.rot / 2 : a.rot;
