@@ -11,10 +11,9 @@
 // i of the four keys. Two such reads make the eight keys of an operand.
 //
 // Tiles are double-buffered: the copies of tile j+1 are issued right after the barrier that
-// opens tile j. They are direct-to-LDS buffer loads; one instruction of a wave copies 1 KB,
-// 4 rows of 128 channels or 8 of 64, which lie on one page, through a descriptor rooted at
-// that row of the page and ending with the sequence: rows behind it, rows of a page that
-// does not exist and channels behind d become zeros. The page numbers of the next 16,384 keys
+// opens tile j. They are direct-to-LDS buffer loads; a wave copies 16 rows, which lie on one
+// page, through a descriptor rooted at the first of them and ending with the sequence: rows
+// behind it, rows of a page that does not exist and channels behind d become zeros. The page numbers of the next 16,384 keys
 // are held in LDS, since a load of them in the loop would wait for the copies.
 //
 // Swizzle: 16-byte chunks of an LDS row are exchanged by an XOR with bits of the row, applied to
@@ -69,24 +68,40 @@ __device__ __forceinline__ int v_swizzle(int row) {
     return (D == 128 ? (row & 3) | (i << 2) : ((row >> 1) & 1) | (i << 1)) << 1;
 }
 
-// One 1 KB copy of K and one of V to LDS. Inline assembly, because the compiler would guard
-// every later LDS read with a wait for all copies in flight; the waits are explicit. M0 is
-// restored, and a wait state separates each write of it from its use.
-__device__ __forceinline__ void copy_pair(const u32x4_t& kd, const u32x4_t& vd, int koff, int voff,
-                                          uint32_t k_lds, uint32_t v_lds) {
+// A wave's copies of one tile to LDS, 1 KB an instruction, to consecutive places. Inline
+// assembly, because the compiler would guard every later LDS read with a wait for all copies in
+// flight; the waits are explicit. M0 is restored, and a wait state separates each write of it
+// from its use.
+template <int NI>
+__device__ __forceinline__ void copy_rows(const u32x4_t& desc, const int (&off)[NI], uint32_t to) {
+    static_assert(NI == 2 || NI == 4, "copies of a wave");
 #if defined(__HIP_DEVICE_COMPILE__)
     uint32_t saved;
-    asm volatile(
-        "s_mov_b32 %[sv], m0\n\t"
-        "s_mov_b32 m0, %[kl]\n\ts_nop 0\n\t"
-        "buffer_load_dwordx4 %[ko], %[kd], 0 offen lds\n\t"
-        "s_mov_b32 m0, %[vl]\n\ts_nop 0\n\t"
-        "buffer_load_dwordx4 %[vo], %[vd], 0 offen lds\n\t"
-        "s_mov_b32 m0, %[sv]"
-        : [sv] "=&s"(saved)
-        : [kl] "s"(k_lds), [vl] "s"(v_lds), [kd] "s"(kd), [vd] "s"(vd), [ko] "v"(koff),
-          [vo] "v"(voff)
-        : "memory");
+    if constexpr (NI == 2)
+        asm volatile(
+            "s_mov_b32 %[sv], m0\n\ts_mov_b32 m0, %[to]\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o0], %[desc], 0 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o1], %[desc], 0 offen lds\n\t"
+            "s_mov_b32 m0, %[sv]"
+            : [sv] "=&s"(saved)
+            : [to] "s"(to), [desc] "s"(desc), [o0] "v"(off[0]), [o1] "v"(off[1])
+            : "memory", "scc");
+    else
+        asm volatile(
+            "s_mov_b32 %[sv], m0\n\ts_mov_b32 m0, %[to]\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o0], %[desc], 0 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o1], %[desc], 0 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o2], %[desc], 0 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %[o3], %[desc], 0 offen lds\n\t"
+            "s_mov_b32 m0, %[sv]"
+            : [sv] "=&s"(saved)
+            : [to] "s"(to), [desc] "s"(desc), [o0] "v"(off[0]), [o1] "v"(off[1]), [o2] "v"(off[2]),
+              [o3] "v"(off[3])
+            : "memory", "scc");
 #endif
 }
 
@@ -121,14 +136,21 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
     const float c2 = a.scale * kLog2e;
     const int shift = __builtin_ctz(c.page);
-    const uint32_t row_bytes = uint32_t(c.d) * 2;
+    const uint32_t row_bytes = uint32_t(c.d) * 2, page_bytes = uint32_t(c.H * c.page) * row_bytes;
+    // (48-bit addresses: the upper 16 bits of a descriptor's address word stay clear)
+    const uint64_t head_at = uint64_t(uint32_t(hk * c.page)) * row_bytes;
+    const uint64_t k_base = (reinterpret_cast<uint64_t>(c.K) & 0xffffffffffffull) + head_at;
+    const uint64_t v_base = (reinterpret_cast<uint64_t>(c.V) & 0xffffffffffffull) + head_at;
+    const uint32_t k_lds = __builtin_amdgcn_readfirstlane(
+        uint32_t(reinterpret_cast<uintptr_t>(&lds[0][0][16 * wave * D])));
 
-    // Source offsets of this lane's copies within an instruction's rows; channels behind d lie
-    // past every descriptor.
+    // A wave copies the 16 rows from 16 * wave on, which lie on one page whatever its size.
+    // Source offsets of this lane's copies from the first of them; channels behind d lie past
+    // every descriptor.
     int koff[NI], voff[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-        const int sub = lane / NCH, row = (n * 4 + wave) * RPI + sub, pc = lane % NCH;
+        const int sub = n * RPI + lane / NCH, row = 16 * wave + sub, pc = lane % NCH;
         const int kc = (pc ^ k_swizzle<D>(row)) * 8, vc = (pc ^ v_swizzle<D>(row)) * 8;
         koff[n] = kc < c.d ? int(sub * row_bytes) + kc * 2 : 0x7ffffff0;
         voff[n] = vc < c.d ? int(sub * row_bytes) + vc * 2 : 0x7ffffff0;
@@ -199,28 +221,20 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
 
             auto issue = [&](int t0, auto buf_c) {
                 constexpr int buf = decltype(buf_c)::value;
-#pragma unroll
-                for (int n = 0; n < NI; ++n) {
-                    const int r0 = (n * 4 + wave) * RPI, key = t0 + r0;
-                    const int p = __builtin_amdgcn_readfirstlane(page_list[(key >> shift) - p0]);
-                    const int live = p < 0 ? 0 : min(max(s.kv - key, 0), RPI);
-                    const uint64_t row = (uint64_t(uint32_t(max(p, 0))) * uint32_t(c.H) + hk) * c.page +
-                                         (key & (c.page - 1));
-                    const uint64_t k_from = reinterpret_cast<uint64_t>(c.K) + row * row_bytes;
-                    const uint64_t v_from = reinterpret_cast<uint64_t>(c.V) + row * row_bytes;
-                    u32x4_t kd, vd;
-                    kd.x = __builtin_amdgcn_readfirstlane(uint32_t(k_from));
-                    kd.y = __builtin_amdgcn_readfirstlane(uint32_t(k_from >> 32) & 0xffffu);
-                    vd.x = __builtin_amdgcn_readfirstlane(uint32_t(v_from));
-                    vd.y = __builtin_amdgcn_readfirstlane(uint32_t(v_from >> 32) & 0xffffu);
-                    kd.z = vd.z = __builtin_amdgcn_readfirstlane(uint32_t(live) * row_bytes);
-                    kd.w = vd.w = 0x00020000u;
-                    copy_pair(kd, vd, koff[n], voff[n],
-                              __builtin_amdgcn_readfirstlane(
-                                  uint32_t(reinterpret_cast<uintptr_t>(&lds[buf][0][r0 * D]))),
-                              __builtin_amdgcn_readfirstlane(
-                                  uint32_t(reinterpret_cast<uintptr_t>(&lds[buf][1][r0 * D]))));
-                }
+                const int key = t0 + 16 * wave;
+                const int p = __builtin_amdgcn_readfirstlane(page_list[(key >> shift) - p0]);
+                const int live = p < 0 ? 0 : min(max(s.kv - key, 0), 16);
+                const uint64_t at = uint64_t(uint32_t(max(p, 0))) * page_bytes +
+                                    uint32_t(key & (c.page - 1)) * row_bytes;
+                u32x4_t desc;
+                desc.z = __builtin_amdgcn_readfirstlane(uint32_t(live) * row_bytes);
+                desc.w = 0x00020000u;
+                desc.x = __builtin_amdgcn_readfirstlane(uint32_t(k_base + at));
+                desc.y = __builtin_amdgcn_readfirstlane(uint32_t((k_base + at) >> 32));
+                copy_rows<NI>(desc, koff, k_lds + buf * 2 * TILE * 2);
+                desc.x = __builtin_amdgcn_readfirstlane(uint32_t(v_base + at));
+                desc.y = __builtin_amdgcn_readfirstlane(uint32_t((v_base + at) >> 32));
+                copy_rows<NI>(desc, voff, k_lds + (buf * 2 + 1) * TILE * 2);
             };
 
             auto step = [&](int t0, auto buf_c) {
