@@ -252,28 +252,41 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 floatx4 sc[2][4];
 #pragma unroll
                 for (int mt = 0; mt < 4; ++mt) sc[0][mt] = sc[1][mt] = floatx4{};
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    bf16x8 ka[4];
+                // Operands are read one step ahead of the products that use them; the barriers
+                // keep the scheduler from sinking a read to its use.
+                bf16x8 ka[2][4];
+                auto k_operands = [&](int kt) {
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt)
-                        ka[mt] = *reinterpret_cast<const bf16x8*>(
+                        ka[kt & 1][mt] = *reinterpret_cast<const bf16x8*>(
                             lk + (k_at ^ (kt << 6)) + (32 * (mt >> 1) + 4 * (mt & 1)) * D * 2);
+                };
+                k_operands(0);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    if (kt + 1 < KT) k_operands(kt + 1);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
-                            sc[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[mt], q[n][kt],
-                                                                                sc[n][mt], 0, 0, 0);
+                            sc[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                ka[kt & 1][mt], q[n][kt], sc[n][mt], 0, 0, 0);
                 }
-                auto v_operand = [&](int t, int dt) {
-                    const char* p = lv + (v_at ^ (dt << 5)) + 32 * t * D * 2;
-                    const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p));
-                    const short4_t y =
-                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * D * 2));
-                    const short8_t z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-                    return __builtin_bit_cast(bf16x8, z);
+                bf16x8 va[2][DT];
+                auto v_operands = [&](int t) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const char* p = lv + (v_at ^ (dt << 5)) + 32 * t * D * 2;
+                        const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p));
+                        const short4_t y =
+                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * D * 2));
+                        va[t][dt] = __builtin_bit_cast(
+                            bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
                 };
+                v_operands(0);
+                __builtin_amdgcn_sched_barrier(0);
 
                 if (bad || t0 + kKeys > lowest) {
 #pragma unroll
@@ -326,14 +339,16 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                         }
                         pb[n] = __builtin_convertvector(p, bf16x8);
                     }
+                    if (t == 0) {
+                        v_operands(1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const bf16x8 va = v_operand(t, dt);
+                    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
-                            acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n],
+                            acc[n][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[t][dt], pb[n],
                                                                                  acc[n][dt], 0, 0, 0);
-                    }
                 }
             };
 
