@@ -262,6 +262,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                             lk + (k_at ^ (kt << 6)) + (32 * (mt >> 1) + 4 * (mt & 1)) * D * 2);
                 };
                 k_operands(0);
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
                     if (kt + 1 < KT) k_operands(kt + 1);
@@ -273,6 +274,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                             sc[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                                 ka[kt & 1][mt], q[n][kt], sc[n][mt], 0, 0, 0);
                 }
+                __builtin_amdgcn_s_setprio(0);
                 bf16x8 va[2][DT];
                 auto v_operands = [&](int t) {
 #pragma unroll
