@@ -1,17 +1,153 @@
 // Attention weight per cached token: w[t] = sum over the rows that see t of
-// exp(scale q.k_t - lse). One wave owns 32 keys (16 of float32) whose K rows stay in its
-// registers as the A operand of the score product S^T = K Q^T, and walks the rows
-// 16 at a time; each lane sums the exponentials of its keys over its column of rows,
-// and the sixteen columns are added once at the end. No two waves add to the same
+// exp(scale q.k_t - lse). A row is (token, head of the group). No two waves add to the same
 // weight, so there are no atomics and the order of a sum depends on the sizes alone.
+//
+// weights_rows_kernel, for up to 32 rows a sequence (a decoding step): Q and lse stay in
+// registers, the workgroup walks a part of the sequence's keys, and what bounds it is reading
+// K. Its waves take the tiles of S^T = K Q^T (paged_tiles.h) in turn, the next one loading
+// while one is computed; each lane sums the exponentials of its keys over its columns of
+// rows, and the sixteen lanes that hold a key's columns are added in a rotation.
+// 64 sequences of 9,000 tokens: 5.3 TB/s, and 4.85 TB/s with a wave per tile and no next one;
+// 64 of 400 to 9,001: 82, 78, 77 and 80 us in parts for 8, 16, 32 and 64 workgroups per CU.
+//
+// weights_keys_kernel, for float32 and more rows: a wave's keys stay in registers and it walks
+// the rows, 16 at a time. (bf16 goes to paged_weights_tiles.hip.)
+#include <algorithm>
+
 #include "paged_plan.h"
 #include "paged_tiles.h"
 
 namespace sparsp {
 namespace {
 
+constexpr int kCus = 256;
+constexpr int kSegment = 16384;  // keys whose page numbers are held at once
+
+// Sum over the 16 lanes of a group, the same in all of them.
+__device__ __forceinline__ float group_sum(float x) {
+#define SPARSP_ROW_ROR(n) \
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xf, 0xf, false))
+    SPARSP_ROW_ROR(8);
+    SPARSP_ROW_ROR(4);
+    SPARSP_ROW_ROR(2);
+    SPARSP_ROW_ROR(1);
+#undef SPARSP_ROW_ROR
+    return x;
+}
+
+// A row's place in Q, its lse in log2 units and the end of the keys it sees (0: none).
+struct Row {
+    int64_t at;
+    float lse2;
+    int limit;
+};
+__device__ __forceinline__ Row row_of(const PagedArgs& a, const Seq& s, int hk, int G, int r) {
+    Row x = {0, 0.f, 0};
+    if (r < s.n * G) {
+        const int i = r / G, h = hk * G + r % G;
+        const float lse = a.lse_in[int64_t(h) * a.tokens + s.q0 + i];
+        x.at = int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token;
+        x.lse2 = lse * kLog2e;
+        x.limit = lse == -INFINITY ? 0 : a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+    }
+    return x;
+}
+
+template <typename T, int D, int NC>
+__global__ __launch_bounds__(256) void weights_rows_kernel(const PagedArgs a, const PagedPlan plan) {
+    using M = TileMath<T, D>;
+    constexpr int KEYS = M::KEYS, JUMP = 4 * KEYS;
+    __shared__ int page_list[kSegment / 16];
+    const sparsp_cache& c = a.cache;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    const auto [bh, part] = unit_of(blockIdx.x, c.B * c.H);
+    const int b = bh / c.H, hk = bh % c.H;
+    const int G = a.q_heads / c.H;
+    const Seq s = sequence(c, a.tokens, b);
+    const int keys = part_keys(plan, s.kv);
+    if (part * int64_t(keys) >= s.kv) return;
+    const int lo = part * keys, end = min(s.kv - lo, keys) + lo;
+    const float c2 = a.scale * kLog2e;
+    const int shift = __builtin_ctz(c.page), mask = c.page - 1;
+
+    // Rows beyond the registers (the caller's max_new was too small) take further rounds, which
+    // add to what the first has written.
+    for (int r0 = 0; r0 == 0 || r0 < s.n * G; r0 += 16 * NC) {
+        const bool add = a.accumulate || r0 > 0;
+        typename M::QTile q[NC];
+        Row row[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const int r = r0 + 16 * n + col;
+            row[n] = row_of(a, s, hk, G, r);
+            M::load_row(q[n], a.Q, row[n].at, r < s.n * G, c.d, lane);
+        }
+        struct Stage {
+            typename M::KTile k;
+            float* to;  // the weight that this lane writes, or NULL
+            float old;
+        };
+        auto load = [&](Stage& st, int t0, int p0) {
+            M::load_k(c, st.k, page_list[((t0 + M::k_group(lane)) >> shift) - p0], hk, t0, lane);
+            st.to = nullptr;
+            st.old = 0.f;
+            const int key = t0 + M::key_of(g, col);
+            if (col < M::PER && key < end) {
+                const int p = page_list[(key >> shift) - p0];
+                if (p >= 0) {
+                    st.to = c.weights + (int64_t(p) * c.H + hk) * c.page + (key & mask);
+                    if (add) st.old = *st.to;
+                }
+            }
+        };
+        auto compute = [&](const Stage& st, int t0) {
+            float w[M::PER] = {};
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                floatx4 sc[M::U];
+                M::scores(st.k, q[n], sc);
+#pragma unroll
+                for (int v = 0; v < M::PER; ++v) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(sc[v / 4][v % 4], c2, -row[n].lse2));
+                    w[v] += t0 + M::key_of(g, v) < row[n].limit ? x : 0.f;
+                }
+            }
+            float mine = 0.f;
+#pragma unroll
+            for (int v = 0; v < M::PER; ++v) {
+                const float sum = group_sum(w[v]);
+                mine = v == col ? sum : mine;
+            }
+            if (st.to) *st.to = st.old + mine;
+        };
+        for (int seg = lo; seg < end; seg += kSegment) {
+            const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
+            const int entries = ((((seg_end + JUMP - 1) & -JUMP) - 1) >> shift) - p0 + 1;
+            __syncthreads();  // the list before has been read
+            for (int e = threadIdx.x; e < entries; e += 256)
+                page_list[e] = page_of(c.table, c.width, c.pages, b, p0 + e);
+            __syncthreads();
+            int t0 = seg + wave * KEYS;
+            if (t0 >= seg_end) continue;
+            Stage A, B;
+            load(A, t0, p0);
+            for (;;) {
+                if (t0 + JUMP < seg_end) load(B, t0 + JUMP, p0);
+                compute(A, t0);
+                t0 += JUMP;
+                if (t0 >= seg_end) break;
+                if (t0 + JUMP < seg_end) load(A, t0 + JUMP, p0);
+                compute(B, t0);
+                t0 += JUMP;
+                if (t0 >= seg_end) break;
+            }
+        }
+    }
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_weights_kernel(const PagedArgs a, int strides) {
+__global__ __launch_bounds__(256) void weights_keys_kernel(const PagedArgs a, int strides) {
     using M = TileMath<T, D>;
     const sparsp_cache& c = a.cache;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -22,66 +158,58 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(const PagedArgs a, i
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
     const float c2 = a.scale * kLog2e;
+    const int shift = __builtin_ctz(c.page);
     constexpr int KEYS = M::KEYS;
     for (int t0 = (first * 4 + wave) * KEYS; t0 < s.kv; t0 += strides * 4 * KEYS) {
         typename M::KTile k;
-        const int page = page_of(c.table, c.width, c.pages, b,
-                                 (t0 + M::k_group(lane)) >> __builtin_ctz(c.page));
+        const int page =
+            page_of(c.table, c.width, c.pages, b, (t0 + M::k_group(lane)) >> shift);
         M::load_k(c, k, page, hk, t0, lane);
         float w[M::PER] = {};
         // Rows before r_first see none of these keys.
         const int r_first = a.causal ? max(0, t0 - (s.kv - s.n)) * G : 0;
         for (int r0 = r_first / 16 * 16; r0 < rows; r0 += 16) {
-            const int r = r0 + col;
+            const Row row = row_of(a, s, hk, G, r0 + col);
             typename M::QTile q;
-            int limit = 0;
-            float lse2 = 0.f;
-            int64_t q_at = 0;
-            if (r < rows) {
-                const int i = r / G, h = hk * G + r % G;
-                q_at = int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token;
-                limit = a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
-                const float l = a.lse_in[int64_t(h) * a.tokens + s.q0 + i];
-                if (l == -INFINITY) limit = 0;
-                lse2 = l * kLog2e;
-            }
-            M::load_row(q, a.Q, q_at, r < rows, c.d, lane);
+            M::load_row(q, a.Q, row.at, r0 + col < rows, c.d, lane);
             floatx4 sc[M::U];
             M::scores(k, q, sc);
 #pragma unroll
             for (int v = 0; v < M::PER; ++v) {
-                const int key = t0 + M::key_of(g, v);
-                const float x = __builtin_amdgcn_exp2f(fmaf(sc[v / 4][v % 4], c2, -lse2));
-                w[v] += key < limit ? x : 0.f;
+                const float x = __builtin_amdgcn_exp2f(fmaf(sc[v / 4][v % 4], c2, -row.lse2));
+                w[v] += t0 + M::key_of(g, v) < row.limit ? x : 0.f;
             }
         }
+        float mine = 0.f;
 #pragma unroll
-        for (int v = 0; v < M::PER; ++v)
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1) w[v] += __shfl_xor(w[v], off);
-        if (col < M::PER) {
-            const int key = t0 + M::key_of(g, col);
-            float mine = 0.f;
-#pragma unroll
-            for (int v = 0; v < M::PER; ++v) mine = v == col ? w[v] : mine;
-            if (key < s.kv) {
-                const int at = page_of(c.table, c.width, c.pages, b, key >> __builtin_ctz(c.page));
-                if (at >= 0) {
-                    float* to = c.weights + (int64_t(at) * c.H + hk) * c.page + (key & (c.page - 1));
-                    *to = a.accumulate ? *to + mine : mine;
-                }
+        for (int v = 0; v < M::PER; ++v) {
+            const float sum = group_sum(w[v]);
+            mine = v == col ? sum : mine;
+        }
+        const int key = t0 + M::key_of(g, col);
+        if (col < M::PER && key < s.kv) {
+            const int at = page_of(c.table, c.width, c.pages, b, key >> shift);
+            if (at >= 0) {
+                float* to = c.weights + (int64_t(at) * c.H + hk) * c.page + (key & (c.page - 1));
+                *to = a.accumulate ? *to + mine : mine;
             }
         }
     }
 }
 
-template <typename T>
-hipError_t launch_t(const PagedArgs& a, int strides, hipStream_t s) {
-    const int grid = a.cache.B * a.cache.H * strides;
+template <typename T, int NC>
+hipError_t launch_rows(const PagedArgs& a, int most_kv, hipStream_t s) {
+    const int pairs = a.cache.B * a.cache.H;
+    const int round = sizeof(T) == 2 ? 128 : 64;  // keys
+    PagedPlan p = {};
+    p.tiles = 1;
+    p.parts = std::max(1, std::min((most_kv + round - 1) / round,
+                                   std::max(1, 32 * kCus / std::min(pairs, 32 * kCus))));
+    p.step = std::max(round, ((most_kv + p.parts - 1) / p.parts + round - 1) / round * round);
     if (a.cache.d <= 64)
-        paged_weights_kernel<T, 64><<<grid, 256, 0, s>>>(a, strides);
+        weights_rows_kernel<T, 64, NC><<<pairs * p.parts, 256, 0, s>>>(a, p);
     else
-        paged_weights_kernel<T, 128><<<grid, 256, 0, s>>>(a, strides);
+        weights_rows_kernel<T, 128, NC><<<pairs * p.parts, 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
@@ -89,17 +217,22 @@ hipError_t launch_t(const PagedArgs& a, int strides, hipStream_t s) {
 
 hipError_t launch_paged_weights(const PagedArgs& a, hipStream_t s) {
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
-    if (a.cache.dtype == SPARSP_BF16 && int64_t(most_new) * (a.q_heads / a.cache.H) > 32)
-        return launch_weights_tiles(a, s);
     const int span = a.cache.width * a.cache.page;
-    const int keys = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
-    const int per = 4 * (a.cache.dtype == SPARSP_BF16 ? 32 : 16);
-    const int64_t pairs = int64_t(a.cache.B) * a.cache.H;
-    int64_t strides = (keys + per - 1) / per;
-    const int64_t most = (int64_t(1) << 22) / pairs;
-    if (strides > most) strides = most < 1 ? 1 : most;
-    return a.cache.dtype == SPARSP_BF16 ? launch_t<uint16_t>(a, int(strides), s)
-                                        : launch_t<float>(a, int(strides), s);
+    const int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
+    const int64_t rows = int64_t(most_new) * (a.q_heads / a.cache.H);
+    const bool bf16 = a.cache.dtype == SPARSP_BF16;
+    if (rows <= 16)
+        return bf16 ? launch_rows<uint16_t, 1>(a, most_kv, s) : launch_rows<float, 1>(a, most_kv, s);
+    if (rows <= 32)
+        return bf16 ? launch_rows<uint16_t, 2>(a, most_kv, s) : launch_rows<float, 2>(a, most_kv, s);
+    if (bf16) return launch_weights_tiles(a, s);
+    const int pairs = a.cache.B * a.cache.H;
+    const int strides = std::max(1, std::min((most_kv + 63) / 64, (1 << 22) / pairs));
+    if (a.cache.d <= 64)
+        weights_keys_kernel<float, 64><<<pairs * strides, 256, 0, s>>>(a, strides);
+    else
+        weights_keys_kernel<float, 128><<<pairs * strides, 256, 0, s>>>(a, strides);
+    return hipGetLastError();
 }
 
 }  // namespace sparsp
