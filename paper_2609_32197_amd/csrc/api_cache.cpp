@@ -165,6 +165,8 @@ int check_query(const sparsp_cache* c, int tokens, const sparsp_rows* Q, float s
         return fail(SPARSP_E_INVALID, "%d query heads are no multiple of H = %d", Q->heads, c->H);
     if (int64_t(c->B) * Q->heads > kMaxPairs)
         return fail(SPARSP_E_UNSUPPORTED, "B * query heads exceeds 2^20");
+    if (int64_t(tokens) * (Q->heads / c->H) > (int64_t(1) << 30))
+        return fail(SPARSP_E_UNSUPPORTED, "tokens * query heads of a key head exceeds 2^30");
     if (!(scale > 0.0f) || scale > 1e30f)
         return fail(SPARSP_E_INVALID, "softmax_scale must be positive and finite");
     if (max_new < 0 || max_kv < 0) return fail(SPARSP_E_INVALID, "max_new or max_kv < 0");

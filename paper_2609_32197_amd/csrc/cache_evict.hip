@@ -540,7 +540,9 @@ hipError_t launch_cache_evict(const sparsp_cache& c, int keep, int first, int re
         e != hipSuccess)
         return e;
     const int row_bytes = c.d * (c.dtype == SPARSP_BF16 ? 2 : 4);
-    const int part = dst_table || row_bytes < kSlice ? row_bytes : kSlice;
+    // (many pairs are work enough, and more workgroups would pass the size of a grid)
+    const bool whole = dst_table || row_bytes < kSlice || c.B * c.H >= 1024;
+    const int part = whole ? row_bytes : kSlice;
     const int slices = (row_bytes + part - 1) / part;
     int lanes = 1;
     while (lanes * 16 < part) lanes *= 2;

@@ -73,9 +73,10 @@ __device__ __forceinline__ void put(Vec<T, V>* p, Vec<T, V> x, bool stream) {
     *p = x;
 }
 
-// A workgroup's places: for each token the byte offset of its row in the pages, or -1. A wave
-// takes a token: new_off is ascending, so the token's sequence is the number of ends
+// A workgroup's places: for each token the byte offset of its row in the pages, kNoPlace, or
+// kNoSequence for a column of no sequence, which nothing is written for. A wave takes a token: new_off is ascending, so the token's sequence is the number of ends
 // new_off[1..B] at or before it, counted 64 at a time.
+constexpr int64_t kNoPlace = -1, kNoSequence = -2;
 template <typename T>
 __device__ __forceinline__ void find_places(const Params& p, int t0, int count, int64_t* place) {
     const sparsp_cache& c = p.cache;
@@ -84,17 +85,18 @@ __device__ __forceinline__ void find_places(const Params& p, int t0, int count, 
         int b = 0;
         for (int e = lane; e < c.B; e += 64) b += c.new_off[e + 1] <= t0 + k;
         for (int off = 32; off; off >>= 1) b += __shfl_xor(b, off);
-        int64_t row = -1;  // of head 0
+        int64_t row = kNoSequence;  // of head 0
         if (b < c.B) {
             const Seq s = sequence(c, p.tokens, b);
             const int i = t0 + k - s.q0, slot = s.kv - s.n + i;
-            if (i >= 0 && i < s.n && slot >= 0) {
+            if (i >= 0 && i < s.n) row = kNoPlace;
+            if (row == kNoPlace && slot >= 0) {
                 const int shift = __builtin_ctz(c.page);
                 const int page = page_of(c.table, c.width, c.pages, b, slot >> shift);
                 if (page >= 0) row = int64_t(page) * c.H * c.page + (slot & (c.page - 1));
             }
         }
-        if (lane == 0) place[k] = row < 0 ? -1 : row * c.d * int64_t(sizeof(T));
+        if (lane == 0) place[k] = row < 0 ? row : row * c.d * int64_t(sizeof(T));
         if (row >= 0 && c.weights)
             for (int h = lane; h < c.H; h += 64) c.weights[row + int64_t(h) * c.page] = 0.f;
     }
@@ -140,6 +142,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const Params p) {
             }
             const char* src = mv.src + int64_t(h) * mv.src_head + int64_t(t0 + k) * mv.src_token;
             char* dst = mv.dst;
+            if (PAGED && place[k] == kNoSequence) continue;
             if (PAGED && mv.paged) {
                 if (place[k] < 0) continue;
                 dst += place[k] + int64_t(h) * p.cache.page * p.d * int64_t(sizeof(T));

@@ -135,6 +135,7 @@ int main() {
         {"in place, other strides", APPEND | ROPE, I, [](Call& x) { x.O = x.Q; x.O.head_stride += 64; }},
         {"out_dtype", ATTEND, T, [](Call& x) { x.out = 5; }},
         {"bf16 from f32", ATTEND, T, [](Call& x) { x.c.dtype = SPARSP_F32; }},
+        {"too many rows", ATTEND | WEIGH, U, [](Call& x) { x.tokens = 1 << 26; x.c.H = 1; x.Q = rows(32); x.O = rows(32); x.O.data = at(14 << 20); }},
         {"scale 0", ATTEND | WEIGH, I, [](Call& x) { x.scale = 0; }},
         {"scale NaN", ATTEND | WEIGH, I, [](Call& x) { x.scale = NAN; }},
         {"scale inf", ATTEND | WEIGH, I, [](Call& x) { x.scale = INFINITY; }},

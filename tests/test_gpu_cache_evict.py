@@ -148,3 +148,9 @@ def test_long_caches(gpu, n, keep, first, recent, page, kind, space):
         assert kept[1, h].tolist() == list(range(lens[1])) + [-1] * (keep - lens[1])
     p1 = table[1].long()
     assert torch.equal(kk[p1], K[p1]) and torch.equal(w2[p1], w[p1])
+
+
+def test_many_short_caches(gpu):
+    """More pairs than the in-place move slices rows for."""
+    bt = R.Batch(53, BF, 8, 8, 64, 16, (0,) * 160, [1 + 7 * b % 61 for b in range(160)])
+    check(bt, 20, 1, 6)

@@ -35,7 +35,9 @@ def test_append(gpu, dtype, Hq, H, d, page, new, kv, bad, order, rot, layout, wi
     kw = {}
     if rot:
         f = torch.from_numpy(sp.sparsp_rope_frequencies(rot)[0])
-        kw = dict(rotary=sp.Rotary(rot, layout), positions=pos.cuda(), inv_freq=f.cuda(), Q=q)
+        q_out = torch.full((Hq, bt.T, d), 7.0, dtype=dtype, device="cuda")
+        kw = dict(rotary=sp.Rotary(rot, layout), positions=pos.cuda(), inv_freq=f.cuda(), Q=q,
+                  Q_out=q_out)
         kr, ktol = R.rotate(k, pos, f, rot, layout, (rot // 2,))
     else:
         kr, ktol = k.double(), torch.zeros(1)
@@ -56,7 +58,10 @@ def test_append(gpu, dtype, Hq, H, d, page, new, kv, bad, order, rot, layout, wi
     if with_weights:
         assert torch.equal(bits(w), bits(want_w))
     if rot:
-        R.close(out, *R.rotate(qf, pos, f, rot, layout, (rot // 2,)), "Q")
+        want, qtol = R.rotate(qf, pos, f, rot, layout, (rot // 2,))
+        want[:, sum(new):] = 7.0  # columns of no sequence: as they were
+        assert out is q_out
+        R.close(out, want, qtol, "Q")
     else:
         assert out is None
 
