@@ -22,7 +22,7 @@ import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
-from . import _SIGNATURES, _RESTYPES, _check, _empty, _torch, BF16, F32, load_library
+from . import _SIGNATURES, _RESTYPES, _check, _torch, BF16, F32, load_library
 
 __all__ = [
     "Rotary",
@@ -151,15 +151,6 @@ def _rows(t, name, index, dtype, tokens, d, heads=None):
     return _ROWS.pack(t.data_ptr() or 16, sh, st, h, 0)
 
 
-def _like_rows(x, dtype=None):
-    """A new tensor in x's order of heads and tokens."""
-    torch = _torch()
-    h, n, d = x.shape
-    if x.stride(1) > x.stride(0):
-        return torch.empty((n, h, d), dtype=dtype or x.dtype, device=x.device).transpose(0, 1)
-    return torch.empty((h, n, d), dtype=dtype or x.dtype, device=x.device)
-
-
 def _call(fn, index, stream, *args):
     """The library call on GPU `index`, which launches need to be current, and its stream."""
     cuda = _torch()._C
@@ -215,7 +206,7 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
                 inverse: bool = False, stream=None):
     """X [heads, tokens, d] rotated to positions [axes, tokens] (or [tokens]); X2 alike.
 
-    Returns Y, or (Y, Y2) with X2. Y may be X (in place). With inverse the transposed rotation:
+    Returns Y (in X's order of heads and tokens, unless given), or (Y, Y2) with X2. Y may be X (in place). With inverse the transposed rotation:
     it turns back (times factor squared), and carries a gradient of Y to one of X.
     """
     torch = _torch()
@@ -225,12 +216,12 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     if X.dim() != 3 or not X.is_cuda:
         raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
     dev, (_, n, d) = X.get_device(), X.shape
-    y = Y if Y is not None else _like_rows(X)
+    y = Y if Y is not None else torch.empty_like(X)
     x, o, count = _rows(X, "X", dev, X.dtype, n, d), _rows(y, "Y", dev, X.dtype, n, d, X.shape[0]), 1
     y2 = None
     if X2 is not None:
         x += _rows(X2, "X2", dev, X.dtype, n, d)
-        y2 = Y2 if Y2 is not None else _like_rows(X2)
+        y2 = Y2 if Y2 is not None else torch.empty_like(X2)
         o += _rows(y2, "Y2", dev, X.dtype, n, d, X2.shape[0])
         count = 2
     elif Y2 is not None:
@@ -282,7 +273,7 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
     if Q is not None:
         q = _rows(Q, "Q", dev, dt, n, d)
         if Q_out is None:
-            Q_out = _like_rows(Q)
+            Q_out = _torch().empty_like(Q)
         qo = _rows(Q_out, "Q_out", dev, dt, n, d, Q.shape[0])
     elif Q_out is not None:
         raise ValueError("Q_out needs Q")
@@ -327,8 +318,10 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     if out_dtype is None:
         out_dtype = _dtype_code(K_cache, "K_cache")
     odt = torch.bfloat16 if out_dtype == BF16 else torch.float32
-    o = O if O is not None else _empty((heads, n, d), odt, Q)
-    ls = lse if lse is not None else _empty((heads, n), torch.float32, Q) if want_lse else None
+    o = O if O is not None else Q.new_empty((heads, n, d), dtype=odt)
+    ls = lse
+    if ls is None and want_lse:
+        ls = Q.new_empty((heads, n), dtype=torch.float32)
     ws, nbytes = None, 0
     if workspace is not None:
         ws = _on(workspace, "workspace", dev)
@@ -379,7 +372,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
     B, H, keep = page_table.shape[0], K_cache.shape[1], int(keep)
     out = kv_len_out if kv_len_out is not None else torch.empty_like(kv_len)
-    lst = kept if kept is not None else _empty((B, H, max(keep, 0)), torch.int32, K_cache)
+    lst = kept if kept is not None else kv_len.new_empty((B, H, max(keep, 0)))
     dst, dst_width = None, 0
     if dst_table is not None:
         if dst_table.dim() != 2 or dst_table.shape[0] != B:
@@ -389,7 +382,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     if workspace is None:
         nbytes = lib.sparsp_cache_evict_workspace_bytes(c)
         if nbytes > 0:
-            workspace = _empty((nbytes,), torch.uint8, K_cache)
+            workspace = K_cache.new_empty((nbytes,), dtype=torch.uint8)
             if stream is not None:
                 workspace.record_stream(stream)
     ws = None if workspace is None else _on(workspace, "workspace", dev)
