@@ -14,6 +14,7 @@
 // output and lse, float32, to the workspace, and a merge kernel joins a row's parts in
 // their order. A sequence short enough for one part writes its output directly.
 #include <algorithm>
+#include <cmath>
 
 #include "paged_plan.h"
 #include "paged_tiles.h"
@@ -255,16 +256,25 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
         for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
         const float base = top == -INFINITY ? 0.f : top;
         float x[4] = {}, total = 0.f;
-        for (int p = group; p < parts; p += 8) {
-            const float w = __builtin_amdgcn_exp2f((lse[p] - base) * kLog2e);
-            total += w;
-            if (ch < c.d) {
-                const float4 y =
-                    *reinterpret_cast<const float4*>(plan.part_o + (at * plan.parts + p) * c.d + ch);
-                x[0] += w * y.x;
-                x[1] += w * y.y;
-                x[2] += w * y.z;
-                x[3] += w * y.w;
+        constexpr int DEEP = 4;  // parts of a group in flight
+        const float* from = plan.part_o + at * plan.parts * c.d + (ch < c.d ? ch : 0);
+        for (int p0 = group; p0 < parts; p0 += 8 * DEEP) {
+            floatx4 y[DEEP];
+            float part[DEEP];
+#pragma unroll
+            for (int u = 0; u < DEEP; ++u) {
+                const int p = min(p0 + 8 * u, parts - 1);
+                y[u] = *reinterpret_cast<const floatx4*>(from + int64_t(p) * c.d);
+                part[u] = lse[p];
+            }
+#pragma unroll
+            for (int u = 0; u < DEEP; ++u) {
+                const float w = p0 + 8 * u < parts
+                                    ? __builtin_amdgcn_exp2f((part[u] - base) * kLog2e)
+                                    : 0.f;
+                total += w;
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) x[q4] += w * y[u][q4];
             }
         }
         __syncthreads();  // the row before has been read
@@ -295,12 +305,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 
 // The launch for what is known of the lengths. bf16 rows of more than 32 a sequence go to
 // the kernel of 128-row tiles; others are taken 16 at a time, or 32 where there are more than
-// 16. The keys are split until there are sixteen workgroups per CU, not for the number of them
-// (two fill a CU) but so that a ragged batch fills the GPU to the end: 64 sequences of 400 to
-// 9,001 tokens take 195 us whole, 155, 150, 142 and 146 us in 2, 4, 8 and 16 parts (64 of 2,560
-// each take 118 us whole and 131 us in 5 parts). A part is at least four rounds of the
-// workgroup's waves, and a cache of up to eight rounds stays whole: the second kernel costs
-// what four rounds cost (613 float32 tokens: 13.8 us whole, 16.4 us in 2 parts). Tiles of 128
+// 16.
+//
+// Parts of the keys, in rounds (a round of a workgroup's waves is 128 keys, 64 of float32). What
+// at most two workgroups a CU do is latency: a round costs about 1 us, and the merge kernel 4 us and about
+// 0.1 us for each part of a row, least in sum at sqrt(10 rounds) parts (one sequence of 8
+// key heads, 1,500 tokens: 13.1 us in 3 parts, 9.5 us in 12; 9,000: 15.8 us in 18, 19.5 us in
+// 71). Up to three rounds stay whole. More workgroups than that makes are split
+// so that a ragged batch fills the GPU to the end, into parts of four rounds and
+// more if there are over eight: 64 sequences of 400 to 9,001 tokens take 195 us whole, 155, 150, 142 and 146 us in 2,
+// 4, 8 and 16 parts (64 of 2,560 each take 118 us whole and 131 us in 5 parts). Tiles of 128
 // rows see keys of like numbers and are split to fill the GPU only (chunks of 1,531 and 2,048
 // tokens, 896 workgroups: 2.12 ms whole, 2.27 ms in 2 parts). There are no more parts than
 // the workspace holds.
@@ -324,14 +338,19 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
     tiles = std::min(tiles, room);
     const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
-    int64_t parts = most_kv <= 8 * round ? 1 : (most_kv + 4 * round - 1) / (4 * round);
-    const int64_t wanted = (r.rows == 128 ? 4 : 16) * kCus;
-    parts = std::min<int64_t>(parts, wanted / std::min<int64_t>(pairs * tiles, wanted));
+    const int64_t rounds = (int64_t(most_kv) + round - 1) / round, units = pairs * tiles;
+    int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
+    if (rounds <= 3) parts = 1;
+    if (units * parts > 2 * kCus) {
+        const int64_t fill = (r.rows == 128 ? 4 : 16) * kCus;
+        parts = rounds <= 8 ? 1 : std::min((rounds + 3) / 4, fill / std::min(units, fill));
+    }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
+    r.plan.step = int((rounds + parts - 1) / parts) * round;
+    if (r.plan.step % 128) r.plan.step += 64;  // (128-row tiles, and the merge, count in 128)
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);
-    r.plan.step = std::max(4 * round, int(((most_kv + parts - 1) / parts + 127) / 128 * 128));
     r.bytes = parts > 1 ? parts * part_bytes : 0;
     return r;
 }
