@@ -327,7 +327,13 @@ __device__ __forceinline__ void first_digit(SelectLds& l, const SplitSpace& sp, 
                                             int want) {
     for (int e = threadIdx.x; e < kBins; e += kThreads) {
         uint32_t sum = 0;
-        for (int g = 0; g < segments; ++g) sum += sp.bins[g * kBins + e];
+        for (int g0 = 0; g0 < segments; g0 += kAhead) {  // (loads of kAhead segments in flight)
+            uint32_t n[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) n[u] = sp.bins[min(g0 + u, segments - 1) * kBins + e];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) sum += g0 + u < segments ? n[u] : 0;
+        }
         l.bins[e] = sum;
     }
     find_digit(l, 11, want);
