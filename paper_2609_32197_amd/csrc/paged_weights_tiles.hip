@@ -32,7 +32,8 @@ __device__ __forceinline__ int q_swizzle(int row) {
     return D == 128 ? row & 15 : (row >> 1) & 7;
 }
 
-template <int D>
+// EVEN: the group's heads divide a tile's rows, so that a thread's rows keep their head.
+template <int D, bool EVEN>
 __global__ __launch_bounds__(256, 2) void weights_tiles_kernel(const PagedArgs a, int strides,
                                                                const Div group) {
     constexpr int NCH = D / 8, KT = D / 32;
@@ -105,16 +106,19 @@ __global__ __launch_bounds__(256, 2) void weights_tiles_kernel(const PagedArgs a
         float next_lse = 0.f;
         int next_limit = 0;
         auto load = [&](int r0) {
+            const bool whole = r0 + kRows <= rows;
 #pragma unroll
             for (int u = 0; u < LOADS; ++u) {
                 // (a row behind the last is read as the first: its exponent is -inf)
-                const bool live = r0 + (u * 256 + tid) / NCH < rows;
-                next[u] = *reinterpret_cast<const u32x4_t*>(live ? from[u] : q0);
+                if (!whole && r0 + (u * 256 + tid) / NCH >= rows) from[u] = q0;
+                next[u] = *reinterpret_cast<const u32x4_t*>(from[u]);
                 from[u] += ahead;
-                head[u] += heads_ahead;
-                if (head[u] >= G) {
-                    head[u] -= G;
-                    from[u] += wrap;
+                if constexpr (!EVEN) {
+                    head[u] += heads_ahead;
+                    if (head[u] >= G) {
+                        head[u] -= G;
+                        from[u] += wrap;
+                    }
                 }
             }
             // (what the load brings is first looked at in keep, behind the tile's products)
@@ -218,10 +222,18 @@ hipError_t launch_weights_tiles(const PagedArgs& a, hipStream_t s) {
     if (strides > most) strides = most < 1 ? 1 : most;
     const Div group = make_div(uint32_t(a.q_heads / a.cache.H));
     const int grid = int(pairs * strides);
-    if (a.cache.d <= 64)
-        weights_tiles_kernel<64><<<grid, 256, 0, s>>>(a, int(strides), group);
-    else
-        weights_tiles_kernel<128><<<grid, 256, 0, s>>>(a, int(strides), group);
+    const bool even = kRows % group.d == 0;
+    if (a.cache.d <= 64) {
+        if (even)
+            weights_tiles_kernel<64, true><<<grid, 256, 0, s>>>(a, int(strides), group);
+        else
+            weights_tiles_kernel<64, false><<<grid, 256, 0, s>>>(a, int(strides), group);
+    } else {
+        if (even)
+            weights_tiles_kernel<128, true><<<grid, 256, 0, s>>>(a, int(strides), group);
+        else
+            weights_tiles_kernel<128, false><<<grid, 256, 0, s>>>(a, int(strides), group);
+    }
     return hipGetLastError();
 }
 
