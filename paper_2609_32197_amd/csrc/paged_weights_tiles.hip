@@ -143,29 +143,38 @@ __global__ __launch_bounds__(256, 2) void weights_tiles_kernel(const PagedArgs a
         // One tile of rows; CROSSED: some rows do not see all of the wave's keys.
         auto tile = [&](int buf, auto crossed_c) {
             constexpr bool CROSSED = decltype(crossed_c)::value;
-#pragma unroll
-            for (int n = 0; n < kRows / 16; ++n) {
+            floatx4 sc[2][4];
+            auto products = [&](int n) {
                 const int row = 16 * n + col;
                 const uint16_t* at = &lds[buf][row * D];
-                floatx4 sc[4] = {};
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sc[n & 1][u] = floatx4{};
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
                     const bf16x8 q = *reinterpret_cast<const bf16x8*>(
                         at + (((4 * kt + g) ^ q_swizzle<D>(row)) * 8));
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u][kt], q, sc[u], 0, 0, 0);
+                        sc[n & 1][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            k[u][kt], q, sc[n & 1][u], 0, 0, 0);
                 }
+            };
+            products(0);
+#pragma unroll
+            for (int n = 0; n < kRows / 16; ++n) {
+                const int row = 16 * n + col;
+                if (n + 1 < kRows / 16) products(n + 1);
                 const float neg = row_neg[buf][row];
                 const int limit = CROSSED ? row_limit[buf][row] - (t0 + 4 * g) : 0;
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float x = __builtin_amdgcn_exp2f(fmaf(sc[u][e], c2, neg));
+                        float x = __builtin_amdgcn_exp2f(fmaf(sc[n & 1][u][e], c2, neg));
                         if (CROSSED) x = 16 * u + e < limit ? x : 0.f;
                         w[u][e] += x;
                     }
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
 
