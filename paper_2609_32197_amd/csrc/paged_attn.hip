@@ -6,8 +6,8 @@
 //
 // paged_rows_kernel, for few rows: a workgroup takes 16 NC rows and a part of the
 // sequence's keys; its four waves walk the key tiles in turn (wave w the tiles w, w+4, ...),
-// each with a softmax of its own, loading the tile after next while they compute. The
-// waves' results are merged in LDS through their running maxima. What bounds it is
+// each with a softmax of its own, the next tile loading while one is computed. The waves'
+// results are merged in LDS through their running maxima. What bounds it is
 // reading K and V, so every tile goes straight to operand registers (paged_tiles.h).
 //
 // Long caches are split: each part (a multiple of `step` keys) writes its normalised
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
                 const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
                 if (whole) {
                     store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch,
-                              a.out_bf16, x);
+                           a.out_bf16, x);
                     if (ch == 0 && a.lse) a.lse[at] = lse;
                 } else {
                     store4(plan.part_o, (at * plan.parts + part) * c.d + ch, false, x);
@@ -233,8 +233,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     }
 }
 
-// Joins the parts of one (token, head): eight groups of 32 lanes take the parts in
-// turn, four channels a lane, and the groups are added in LDS in their order.
+// Joins the parts of rows (token, head). 32 lanes hold a row, four channels a lane. SHARED, for few
+// rows: the eight groups of a workgroup take one row's parts in turn and are added in LDS in
+// their order. Otherwise each group has a row of its own (16,384 rows of two parts: 27 us with
+// the attention, 50 us with a workgroup for each row).
+template <bool SHARED>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, const PagedPlan plan,
                                                           int per_head) {
     __shared__ float part_x[8][128];
@@ -246,30 +249,32 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     const int keys = part_keys(plan, s.kv);
     if (s.kv <= keys) return;
     const int parts = (s.kv + keys - 1) / keys;
-    const int group = threadIdx.x >> 5, ch = (threadIdx.x & 31) * 4;
-    for (int i = blockIdx.x % per_head; i < s.n; i += per_head) {
+    const int group = threadIdx.x >> 5, lane = threadIdx.x & 31, ch = lane * 4;
+    const int first = SHARED ? group : 0, stride = SHARED ? 8 : 1;  // of a group's parts
+    constexpr int ROWS = SHARED ? 1 : 8, DEEP = 4;                  // DEEP parts in flight
+    for (int i0 = blockIdx.x % per_head * ROWS; i0 < s.n; i0 += per_head * ROWS) {
+        const int i = SHARED ? i0 : min(i0 + group, s.n - 1);
         const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
         const float* lse = plan.part_lse + at * plan.parts;
         float top = -INFINITY;
-        for (int p = threadIdx.x & 63; p < parts; p += 64) top = fmaxf(top, lse[p]);
+        for (int p = lane; p < parts; p += 32) top = fmaxf(top, lse[p]);
 #pragma unroll
-        for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+        for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
         const float base = top == -INFINITY ? 0.f : top;
         float x[4] = {}, total = 0.f;
-        constexpr int DEEP = 4;  // parts of a group in flight
         const float* from = plan.part_o + at * plan.parts * c.d + (ch < c.d ? ch : 0);
-        for (int p0 = group; p0 < parts; p0 += 8 * DEEP) {
+        for (int p0 = first; p0 < parts; p0 += stride * DEEP) {
             floatx4 y[DEEP];
             float part[DEEP];
 #pragma unroll
             for (int u = 0; u < DEEP; ++u) {
-                const int p = min(p0 + 8 * u, parts - 1);
+                const int p = min(p0 + stride * u, parts - 1);
                 y[u] = *reinterpret_cast<const floatx4*>(from + int64_t(p) * c.d);
                 part[u] = lse[p];
             }
 #pragma unroll
             for (int u = 0; u < DEEP; ++u) {
-                const float w = p0 + 8 * u < parts
+                const float w = p0 + stride * u < parts
                                     ? __builtin_amdgcn_exp2f((part[u] - base) * kLog2e)
                                     : 0.f;
                 total += w;
@@ -277,12 +282,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
                 for (int q4 = 0; q4 < 4; ++q4) x[q4] += w * y[u][q4];
             }
         }
-        __syncthreads();  // the row before has been read
+        if constexpr (SHARED) {
+            __syncthreads();  // the row before has been read
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) part_x[group][ch + q4] = x[q4];
-        if (ch == 0) part_w[group] = total;
-        __syncthreads();
-        if (group == 0) {
+            for (int q4 = 0; q4 < 4; ++q4) part_x[group][ch + q4] = x[q4];
+            if (ch == 0) part_w[group] = total;
+            __syncthreads();
+            if (group > 0) continue;
             total = 0.f;
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) x[q4] = 0.f;
@@ -292,14 +298,15 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) x[q4] += part_x[w][ch + q4];
             }
-            const bool any = total > 0.f;
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] / total : 0.f;
-            if (ch < c.d)
-                store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch,
-                              a.out_bf16, x);
-            if (ch == 0 && a.lse) a.lse[at] = any ? top + __logf(total) : -INFINITY;
+        } else if (i0 + group >= s.n) {
+            continue;
         }
+        const bool any = total > 0.f;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] / total : 0.f;
+        if (ch < c.d)
+            store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch, a.out_bf16, x);
+        if (ch == 0 && a.lse) a.lse[at] = any ? top + __logf(total) : -INFINITY;
     }
 }
 
@@ -308,16 +315,18 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 // 16.
 //
 // Parts of the keys, in rounds (a round of a workgroup's waves is 128 keys, 64 of float32). What
-// at most two workgroups a CU do is latency: a round costs about 1 us, and the merge kernel 4 us and about
-// 0.1 us for each part of a row, least in sum at sqrt(10 rounds) parts (one sequence of 8
-// key heads, 1,500 tokens: 13.1 us in 3 parts, 9.5 us in 12; 9,000: 15.8 us in 18, 19.5 us in
-// 71). Up to three rounds stay whole. More workgroups than that makes are split
-// so that a ragged batch fills the GPU to the end, into parts of four rounds and
-// more if there are over eight: 64 sequences of 400 to 9,001 tokens take 195 us whole, 155, 150, 142 and 146 us in 2,
-// 4, 8 and 16 parts (64 of 2,560 each take 118 us whole and 131 us in 5 parts). Tiles of 128
-// rows see keys of like numbers and are split to fill the GPU only (chunks of 1,531 and 2,048
-// tokens, 896 workgroups: 2.12 ms whole, 2.27 ms in 2 parts). There are no more parts than
-// the workspace holds.
+// at most two workgroups a CU do is latency: a round costs about 1 us, the merge kernel 4 us and
+// about 0.1 us for each part of a row, least in sum at sqrt(10 rounds) parts (one sequence of
+// 8 key heads, 1,500 tokens: 13.1 us in 3 parts, 9.5 us in 12; 9,000: 15.8 us in 18, 19.5 us
+// in 71). Up to three rounds stay whole, and tiles of 128 rows, whose partial rows are many, up
+// to seven (512 new tokens of 32 heads over 512: 20 us whole, 26 us in 4 parts).
+//
+// More workgroups than that makes are split so that a ragged batch fills the GPU to the end,
+// into parts of four rounds and more if there are over eight: 64 sequences of 400 to 9,001
+// tokens take 195 us whole, 155, 150, 142 and 146 us in 2, 4, 8 and 16 parts (64 of 2,560 each
+// take 118 us whole and 131 us in 5 parts). Tiles of 128 rows see keys of like numbers and
+// fill the GPU once, two workgroups a CU (1,000 tokens of 16 heads over 8,000: 212 us whole, 81 us
+// in 4 parts, 93 us in 8). There are no more parts than the workspace holds.
 struct Shape {
     PagedPlan plan;
     int rows;       // of a tile
@@ -340,15 +349,14 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
     const int64_t rounds = (int64_t(most_kv) + round - 1) / round, units = pairs * tiles;
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
-    if (rounds <= 3) parts = 1;
+    if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, units * parts / 128) : 0)) parts = 1;
     if (units * parts > 2 * kCus) {
-        const int64_t fill = (r.rows == 128 ? 4 : 16) * kCus;
+        const int64_t fill = (r.rows == 128 ? 2 : 16) * kCus;
         parts = rounds <= 8 ? 1 : std::min((rounds + 3) / 4, fill / std::min(units, fill));
     }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
     r.plan.step = int((rounds + parts - 1) / parts) * round;
-    if (r.plan.step % 128) r.plan.step += 64;  // (128-row tiles, and the merge, count in 128)
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);
     r.bytes = parts > 1 ? parts * part_bytes : 0;
@@ -389,8 +397,13 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
     if (e != hipSuccess || r.plan.parts == 1) return e;
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
     const int64_t pairs = int64_t(a.cache.B) * a.q_heads;
-    const int64_t per = std::min<int64_t>(most_new, std::max<int64_t>(1, (int64_t(1) << 22) / pairs));
-    paged_merge_kernel<<<int(pairs * per), 256, 0, s>>>(a, r.plan, int(per));
+    const bool shared = pairs * most_new <= 16 * kCus;
+    const int64_t runs = shared ? most_new : (most_new + 7) / 8;  // workgroups of a head
+    const int per = int(std::min(runs, std::max<int64_t>(1, (int64_t(1) << 22) / pairs)));
+    if (shared)
+        paged_merge_kernel<true><<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
+    else
+        paged_merge_kernel<false><<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
     return hipGetLastError();
 }
 
