@@ -4,11 +4,12 @@
 // group), token-major: n new tokens of a group of G heads are n G rows, packed 16 to an
 // operand. A decoding step of G = 4 thus reads K and V once for four rows.
 //
-// paged_rows_kernel, for few rows: a workgroup takes 16 NC rows and a part of the
-// sequence's keys; its four waves walk the key tiles in turn (wave w the tiles w, w+4, ...),
-// each with a softmax of its own, the next tile loading while one is computed. The waves'
-// results are merged in LDS through their running maxima. What bounds it is
-// reading K and V, so every tile goes straight to operand registers (paged_tiles.h).
+// paged_rows_kernel, for few rows a sequence and for float32: a workgroup takes 16 NC rows and
+// a part of the sequence's keys; its four waves walk the key tiles in turn (wave w the tiles
+// w, w+4, ...), each with a softmax of its own, the next tile loading while one is computed.
+// The waves' results are merged in LDS through their running maxima. What bounds it is reading
+// K and V, so every tile goes straight to operand registers (paged_tiles.h). More bf16 rows go
+// to paged_attn_tiles.hip.
 //
 // Long caches are split: each part (a multiple of `step` keys) writes its normalised
 // output and lse, float32, to the workspace, and a merge kernel joins a row's parts in
@@ -310,9 +311,12 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     }
 }
 
-// The launch for what is known of the lengths. bf16 rows of more than 32 a sequence go to
-// the kernel of 128-row tiles; others are taken 16 at a time, or 32 where there are more than
-// 16.
+// The launch for what is known of the lengths. bf16 rows of more than 16 a sequence go to
+// the kernel of 128-row tiles (d = 128: 32 sequences of 8,000, 32 rows each: 237 us 32 rows at
+// a time from registers, 198 us; one of 2,000 with 24 rows 13.0 and 15.3 us). At d <= 64, where
+// a row's operands take half the registers, those of more than 32 do (64 sequences of 400 to
+// 4,000, 24 rows each: 34.6 us from registers, 38.0 us by the tiles). float32 rows are taken 16
+// or 32 at a time.
 //
 // Parts of the keys, in rounds (a round of a workgroup's waves is 128 keys, 64 of float32). What
 // at most two workgroups a CU do is latency: a round costs about 1 us, the merge kernel 4 us and
@@ -321,12 +325,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 // in 71). Up to three rounds stay whole, and tiles of 128 rows, whose partial rows are many, up
 // to seven (512 new tokens of 32 heads over 512: 20 us whole, 26 us in 4 parts).
 //
-// More workgroups than that makes are split so that a ragged batch fills the GPU to the end,
-// into parts of four rounds and more if there are over eight: 64 sequences of 400 to 9,001
-// tokens take 195 us whole, 155, 150, 142 and 146 us in 2, 4, 8 and 16 parts (64 of 2,560 each
-// take 118 us whole and 131 us in 5 parts). Tiles of 128 rows see keys of like numbers and
-// fill the GPU once, two workgroups a CU (1,000 tokens of 16 heads over 8,000: 212 us whole, 81 us
-// in 4 parts, 93 us in 8). There are no more parts than the workspace holds.
+// More workgroups than that makes are split until two a CU have work, into parts of four rounds
+// and more if there are over eight (1,000 tokens of 16 heads over 8,000: 212 us whole, 81 us in
+// 4 parts, which is that, and 93 us in 8). Few rows a sequence are split further, into parts of
+// sixteen rounds, so that a ragged batch fills the GPU to the end: 64 sequences of 400 to 9,001
+// tokens, 4 rows each, take 195 us whole and 140 us in 5 parts, with 40 rows 221 us in one and
+// 162 us in 5 (32 of 8,000 each, which gain nothing by it, 192 and 198 us). Rows of more than 64
+// do not gain (128 each: 229 us either way; 32 of 8,000: 209 us in 2 parts, 243 us in 4). There
+// are no more parts than the workspace holds.
 struct Shape {
     PagedPlan plan;
     int rows;       // of a tile
@@ -341,7 +347,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
     Shape r = {};
     const int64_t rows = int64_t(most_new) * G;
-    r.rows = rows <= 16 ? 16 : rows <= 32 || c.dtype == SPARSP_F32 ? 32 : 128;
+    r.rows = rows <= 16 ? 16 : c.dtype == SPARSP_F32 || (rows <= 32 && c.d <= 64) ? 32 : 128;
     int64_t tiles = (rows + r.rows - 1) / r.rows;
     const int64_t pairs = int64_t(c.B) * c.H;
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
@@ -351,8 +357,10 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
     if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, units * parts / 128) : 0)) parts = 1;
     if (units * parts > 2 * kCus) {
-        const int64_t fill = (r.rows == 128 ? 2 : 16) * kCus;
-        parts = rounds <= 8 ? 1 : std::min((rounds + 3) / 4, fill / std::min(units, fill));
+        const int64_t fill = 2 * kCus / std::min<int64_t>(units, 2 * kCus);
+        const int64_t level = 16 * kCus / std::min<int64_t>(units, 16 * kCus);
+        parts = rows > 64 ? fill : std::max(fill, std::min(level, (rounds + 15) / 16));
+        parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
     }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
@@ -370,13 +378,16 @@ hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_type(const PagedArgs& a, const Shape& r, hipStream_t s) {
-    if (a.cache.d <= 64)
-        return r.rows == 16 ? launch_rows<T, 64, 1>(a, r.plan, s)
-                            : launch_rows<T, 64, 2>(a, r.plan, s);
-    return r.rows == 16 ? launch_rows<T, 128, 1>(a, r.plan, s)
-                        : launch_rows<T, 128, 2>(a, r.plan, s);
+hipError_t launch_few(const PagedArgs& a, const Shape& r, hipStream_t s) {
+    const bool small = a.cache.d <= 64, few = r.rows == 16;
+    if (a.cache.dtype == SPARSP_BF16)
+        return !small ? launch_rows<uint16_t, 128, 1>(a, r.plan, s)
+               : few  ? launch_rows<uint16_t, 64, 1>(a, r.plan, s)
+                      : launch_rows<uint16_t, 64, 2>(a, r.plan, s);
+    if (few)
+        return small ? launch_rows<float, 64, 1>(a, r.plan, s)
+                     : launch_rows<float, 128, 1>(a, r.plan, s);
+    return small ? launch_rows<float, 64, 2>(a, r.plan, s) : launch_rows<float, 128, 2>(a, r.plan, s);
 }
 
 }  // namespace
@@ -391,9 +402,7 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
         r.plan.part_o = static_cast<float*>(a.ws);
         r.plan.part_lse = r.plan.part_o + int64_t(a.q_heads) * a.tokens * r.plan.parts * a.cache.d;
     }
-    hipError_t e = r.rows == 128                   ? launch_paged_tiles(a, r.plan, s)
-                   : a.cache.dtype == SPARSP_BF16 ? launch_type<uint16_t>(a, r, s)
-                                                  : launch_type<float>(a, r, s);
+    const hipError_t e = r.rows == 128 ? launch_paged_tiles(a, r.plan, s) : launch_few(a, r, s);
     if (e != hipSuccess || r.plan.parts == 1) return e;
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
     const int64_t pairs = int64_t(a.cache.B) * a.q_heads;
