@@ -30,6 +30,7 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
 
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -41,6 +42,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 constexpr int kPages = 8192;       // page numbers held in LDS
 constexpr int kCandidates = 4096;  // keys held in LDS
 constexpr int kAhead = 8;          // loads of a lane in flight
+constexpr int kSegments = 32;      // workgroups for a (sequence, head) at most
 
 struct SelectLds {
     uint32_t bins[kBins];
@@ -280,21 +282,23 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const sparsp_cache c, 
 }
 
 // The same by `segments` workgroups for each (sequence, head), in three launches. Workspace of
-// a pair: the segments' counts by first digit [segments][2048], what a segment has {above the
-// digit, at it} [segments][2], and the keys at it [segments][span].
+// a pair: the segments' counts by first digit [segments][2048], {the first digit of T, keys
+// above it}, what a segment has {above the digit, at it} [segments][2], and the keys at it
+// [segments][span].
 struct SplitSpace {
     uint32_t* bins;
+    uint32_t* digit;
     int* counts;
     uint32_t* keys;
     int span;  // keys of a segment at most
 };
 __host__ __device__ __forceinline__ int64_t split_words(int segments, int64_t span) {
-    return segments * (int64_t(kBins) + 2 + span);
+    return segments * (int64_t(kBins) + 2 + span) + 2;
 }
 __device__ __forceinline__ SplitSpace split_space(uint32_t* ws, int pair, int segments, int span) {
     uint32_t* p = ws + pair * split_words(segments, span);
-    return {p, reinterpret_cast<int*>(p + int64_t(segments) * kBins),
-            p + int64_t(segments) * (kBins + 2), span};
+    uint32_t* digit = p + int64_t(segments) * kBins;
+    return {p, digit, reinterpret_cast<int*>(digit + 2), digit + 2 + 2 * segments, span};
 }
 
 template <bool WIDE>
@@ -325,17 +329,21 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const sparsp_cache c, i
 // The first digit of T from the segments' counts, into found.
 __device__ __forceinline__ void first_digit(SelectLds& l, const SplitSpace& sp, int segments,
                                             int want) {
-    for (int e = threadIdx.x; e < kBins; e += kThreads) {
-        uint32_t sum = 0;
-        for (int g0 = 0; g0 < segments; g0 += kAhead) {  // (loads of kAhead segments in flight)
-            uint32_t n[kAhead];
+    static_assert(kBins == 2 * kThreads);
+    const int e = 2 * threadIdx.x;
+    u32x2_t sum = {};
+    for (int g0 = 0; g0 < segments; g0 += 2 * kAhead) {  // (loads of 16 segments in flight)
+        u32x2_t n[2 * kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) n[u] = sp.bins[min(g0 + u, segments - 1) * kBins + e];
+        for (int u = 0; u < 2 * kAhead; ++u)
+            n[u] = *reinterpret_cast<const u32x2_t*>(sp.bins +
+                                                     min(g0 + u, segments - 1) * kBins + e);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) sum += g0 + u < segments ? n[u] : 0;
-        }
-        l.bins[e] = sum;
+        for (int u = 0; u < 2 * kAhead; ++u)
+            if (g0 + u < segments) sum += n[u];
     }
+    l.bins[e] = sum.x;
+    l.bins[e + 1] = sum.y;
     find_digit(l, 11, want);
 }
 
@@ -367,6 +375,10 @@ __global__ __launch_bounds__(kThreads) void gather_keys_kernel(const sparsp_cach
     if (threadIdx.x == 0) {
         sp.counts[2 * segment] = l.wave_gt[0];
         sp.counts[2 * segment + 1] = l.candidates;
+        if (segment == 0) {
+            sp.digit[0] = l.found[0];
+            sp.digit[1] = l.found[1];
+        }
     }
 }
 
@@ -381,35 +393,56 @@ __global__ __launch_bounds__(kThreads) void place_kernel(const sparsp_cache c, i
     if (!choice_of(c, pair, keep, first, recent, &x)) return;
     const int shift = __builtin_ctz(c.page), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Segment s = segment_of(x, segment, segments, shift);
-    list_pages(c, l, x, s, shift);
     const SplitSpace sp = split_space(ws, pair, segments, span);
-    int want = x.want;
-    first_digit(l, sp, segments, want);
-    uint32_t T = l.found[0] << 21;
-    want -= int(l.found[1]);
-    auto every_key = [&](auto f) {  // f(segment, key); a wave takes a segment
-        for (int g = wave; g < segments; g += kWaves) {
-            const int count = sp.counts[2 * g + 1];
-            for (int e = lane; e < count; e += 64) f(g, sp.keys[int64_t(g) * span + e]);
+    uint32_t T = sp.digit[0] << 21;
+    int want = x.want - int(sp.digit[1]);
+    // A wave has the keys of two segments, the first 512 of each in registers, all asked for
+    // at once.
+    constexpr int OWN = kSegments / kWaves;
+    int count[OWN];
+    uint32_t key[OWN][kAhead];
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const int g = wave + j * kWaves;
+        count[j] = g < segments ? sp.counts[2 * g + 1] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < OWN; ++j)
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            key[j][u] = lane + 64 * u < count[j]
+                            ? sp.keys[int64_t(wave + j * kWaves) * span + lane + 64 * u]
+                            : 0;
+    auto every_key = [&](auto f) {  // f(is it of a segment before, key)
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const int g = wave + j * kWaves;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (lane + 64 * u < count[j]) f(g < segment, key[j][u]);
+            for (int e = 64 * kAhead + lane; e < count[j]; e += 64)
+                f(g < segment, sp.keys[int64_t(g) * span + e]);
         }
     };
+    list_pages(c, l, x, s, shift);
+    clear_bins(l);
+    __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
         const int high = pass ? 10 : 21, low = pass ? 0 : 10, bits = high - low;
-        clear_bins(l);
-        __syncthreads();
-        every_key([&](int, uint32_t k) {
+        every_key([&](bool, uint32_t k) {
             if (k >> high == T >> high) atomicAdd(&l.bins[(k >> low) & ((1u << bits) - 1)], 1u);
         });
         find_digit(l, bits, want);
         T |= l.found[0] << low;
         want -= int(l.found[1]);
-        __syncthreads();  // found is rewritten by the next pass
+        clear_bins(l);
+        __syncthreads();
     }
     if (threadIdx.x < 2) before[threadIdx.x] = 0;
     __syncthreads();
-    every_key([&](int g, uint32_t k) {
-        if (g < segment && k > T) atomicAdd(&before[0], 1);
-        if (g < segment && k == T) atomicAdd(&before[1], 1);
+    every_key([&](bool earlier, uint32_t k) {
+        if (earlier && k > T) atomicAdd(&before[0], 1);
+        if (earlier && k == T) atomicAdd(&before[1], 1);
     });
     if (int(threadIdx.x) < segment) atomicAdd(&before[0], sp.counts[2 * threadIdx.x]);
     int above = 0, eq = 0;
@@ -504,7 +537,7 @@ namespace {
 int segments_of(const sparsp_cache& c) {
     const int64_t tokens = int64_t(c.width) * c.page, pairs = int64_t(c.B) * c.H;
     if (tokens <= 16384 || pairs > 64) return 1;
-    return int(std::min<int64_t>({32, 128 / pairs, tokens / 4096}));
+    return int(std::min<int64_t>({kSegments, 128 / pairs, tokens / 4096}));
 }
 int64_t segment_span(const sparsp_cache& c, int segments) {
     const int64_t groups = int64_t(c.width) * c.page / 64 + 2;
