@@ -350,7 +350,8 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     r.rows = rows <= 16 ? 16 : c.dtype == SPARSP_F32 || (rows <= 32 && c.d <= 64) ? 32 : 128;
     int64_t tiles = (rows + r.rows - 1) / r.rows;
     const int64_t pairs = int64_t(c.B) * c.H;
-    const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / pairs);
+    // (a grid holds fewer than 2^32 threads, and units are rounded up to the eight XCDs)
+    const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / std::max<int64_t>(pairs, 8));
     tiles = std::min(tiles, room);
     const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
     const int64_t rounds = (int64_t(most_kv) + round - 1) / round, units = pairs * tiles;

@@ -225,3 +225,28 @@ def test_another_stream(gpu):
     wO, wL, tO, tL = R.attention(bt)
     R.close(lse, wL, tL)
     R.close(O, wO, tO)
+
+
+def test_more_row_tiles_than_a_grid_holds(gpu):
+    """2^26 rows of one key head are 2^21 tiles of 32 rows."""
+    n, kv, d = 1 << 25, 40, 4
+    g = torch.Generator(device="cuda").manual_seed(31)
+    Q = torch.randn((2, n, d), generator=g, device="cuda")
+    K, V = (torch.randn((3, 1, 16, d), generator=g, device="cuda") for _ in range(2))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    O, lse = sp.sparsp_paged_attn(Q, K, V, torch.tensor([[2, 0, 1]], **i32),
+                                  torch.tensor([0, n], **i32), torch.tensor([kv], **i32),
+                                  causal=False)
+    k, v = (x.cpu()[[2, 0, 1], 0].reshape(48, d)[:kv].double() for x in (K, V))
+    at = torch.cat([torch.arange(0, n, 9973, device="cuda"), torch.arange(n - 40, n, device="cuda")])
+    q = Q[:, at].cpu().double()
+    s = 0.5 * (q[:, :, None, :] * k).sum(-1)
+    p = torch.softmax(s, -1)
+    e = 0.5 * (d + 16) * R.U * (q.abs()[:, :, None, :] * k.abs()).sum(-1).amax(-1)
+    tL = 2 * e + (kv + 64) * R.U + 2.0 ** -19 + 4 * R.U * torch.logsumexp(s, -1).abs()
+    R.close(lse[:, at], torch.logsumexp(s, -1), tL, "lse")
+    w = (p[..., None] * v).sum(-2)
+    A = (p[..., None] * v.abs()).sum(-2)
+    tO = A * (4 * e[..., None] + 2 * (kv + 64) * R.U + 2.0 ** -18) + R.U * w.abs()
+    R.close(O[:, at], w, tO, "O")
+    assert torch.isfinite(O).all()
