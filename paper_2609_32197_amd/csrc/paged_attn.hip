@@ -327,12 +327,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 //
 // More workgroups than that makes are split until two a CU have work, into parts of four rounds
 // and more if there are over eight (1,000 tokens of 16 heads over 8,000: 212 us whole, 81 us in
-// 4 parts, which is that, and 93 us in 8). Few rows a sequence are split further, into parts of
-// sixteen rounds, so that a ragged batch fills the GPU to the end: 64 sequences of 400 to 9,001
-// tokens, 4 rows each, take 195 us whole and 140 us in 5 parts, with 40 rows 221 us in one and
-// 162 us in 5 (32 of 8,000 each, which gain nothing by it, 192 and 198 us). Rows of more than 64
-// do not gain (128 each: 229 us either way; 32 of 8,000: 209 us in 2 parts, 243 us in 4). There
-// are no more parts than the workspace holds.
+// 4 parts, which is that, and 93 us in 8); into four times as many where that leaves a quarter
+// of the GPU empty (675 tokens of 32 heads over 24,153: 172 tiles, 283 us in 2 parts, 242 us in
+// 8). Few rows a sequence, and float32, whose products take 8 times as long as bf16's while a
+// merge costs the same, are split further, into parts of sixteen rounds (float32: eight), so
+// that a ragged batch fills the GPU to the end: 64 sequences of 400 to 9,001 tokens, 4 rows each,
+// take 195 us whole and 140 us in 5 parts, with 40 rows 221 us in one and 162 us in 5 (32 of
+// 8,000 each, which gain nothing by it, 192 and 198 us); float32, 710 to 279 tokens of 5
+// sequences over 5,671 to 9,606: 1,330 us whole, 984 us. bf16 rows of more than 64 do not gain
+// (128 each: 229 us either way; 32 of 8,000: 209 us in 2 parts, 243 us in 4). There are no more
+// parts than the workspace holds.
 struct Shape {
     PagedPlan plan;
     int rows;       // of a tile
@@ -358,9 +362,15 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
     if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, units * parts / 128) : 0)) parts = 1;
     if (units * parts > 2 * kCus) {
-        const int64_t fill = 2 * kCus / std::min<int64_t>(units, 2 * kCus);
-        const int64_t level = 16 * kCus / std::min<int64_t>(units, 16 * kCus);
-        parts = rows > 64 ? fill : std::max(fill, std::min(level, (rounds + 15) / 16));
+        // (of the tiles of the longest sequence, those that all the new tokens can fill)
+        const int64_t live = std::min(units, c.H * (a.tokens * int64_t(G) / r.rows + c.B));
+        int64_t fill = 2 * kCus / std::min<int64_t>(live, 2 * kCus);
+        if (rounds >= 16 && live < 2 * kCus && live * fill < 3 * kCus / 2) fill *= 4;
+        const int64_t level = 16 * kCus / std::min<int64_t>(live, 16 * kCus);
+        const int64_t least = c.dtype == SPARSP_F32 ? 8 : 16;  // rounds of a part
+        parts = r.rows == 128 && rows > 64
+                    ? fill
+                    : std::max(fill, std::min(level, (rounds + least - 1) / least));
         parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
     }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
