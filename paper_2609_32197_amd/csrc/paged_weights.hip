@@ -10,8 +10,15 @@
 // 64 sequences of 9,000 tokens: 5.3 TB/s, and 4.85 TB/s with a wave per tile and no next one;
 // 64 of 400 to 9,001: 82, 78, 77 and 80 us in parts for 8, 16, 32 and 64 workgroups per CU.
 //
-// weights_keys_kernel, for float32 and more rows: a wave's keys stay in registers and it walks
-// the rows, 16 at a time. (bf16 goes to paged_weights_tiles.hip.)
+// weights_keys_kernel, for more rows, float32 or few keys: a wave's keys stay in registers and it
+// walks the rows, 16 at a time, the next ones loading while some are computed. The rows
+// come from cache; float32 is bound by the matrix pipe. SPLIT shares the rows out to the four
+// waves instead of the keys: four times the workgroups. bf16 does so where that makes up to two
+// workgroups a CU, and goes to paged_weights_tiles.hip otherwise (32 heads of 128, 2,000 tokens
+// over as many: 91 us, 178 us by its 64 workgroups; 1,000 over 4,000: 78 and 100 us; 16 heads
+// of 4 sequences, 1,000 over 1,000, four a CU: 45 and 32 us). float32 does where the keys do not
+// fill the GPU, and for 2,048 rows and more, whose tail it evens out (32 heads, 300 tokens over
+// 300: 26 us, 76 us; 2,000 over 2,000: 373 and 511 us; 64 over 8,000: 87 and 80 us).
 #include <algorithm>
 
 #include "paged_plan.h"
@@ -146,55 +153,116 @@ __global__ __launch_bounds__(256) void weights_rows_kernel(const PagedArgs a, co
     }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void weights_keys_kernel(const PagedArgs a, int strides) {
+// SPLIT: the waves share their keys and take the groups of 16 rows in turn; their sums are added
+// in LDS in the waves' order.
+template <typename T, int D, int NK, bool SPLIT>
+__global__ __launch_bounds__(256) void weights_keys_kernel(const PagedArgs a, int strides,
+                                                           const Div group) {
     using M = TileMath<T, D>;
+    constexpr int KEYS = M::KEYS, MINE = NK * KEYS, ALL = SPLIT ? MINE : 4 * MINE;
+    __shared__ float sums[4][MINE];
     const sparsp_cache& c = a.cache;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, g = lane >> 4;
     const int bh = blockIdx.x / strides, first = blockIdx.x % strides;
     const int b = bh / c.H, hk = bh % c.H;
-    const int G = a.q_heads / c.H;
+    const int G = int(group.d);
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
     const float c2 = a.scale * kLog2e;
-    const int shift = __builtin_ctz(c.page);
-    constexpr int KEYS = M::KEYS;
-    for (int t0 = (first * 4 + wave) * KEYS; t0 < s.kv; t0 += strides * 4 * KEYS) {
-        typename M::KTile k;
-        const int page =
-            page_of(c.table, c.width, c.pages, b, (t0 + M::k_group(lane)) >> shift);
-        M::load_k(c, k, page, hk, t0, lane);
-        float w[M::PER] = {};
-        // Rows before r_first see none of these keys.
-        const int r_first = a.causal ? max(0, t0 - (s.kv - s.n)) * G : 0;
-        for (int r0 = r_first / 16 * 16; r0 < rows; r0 += 16) {
-            const Row row = row_of(a, s, hk, G, r0 + col);
-            typename M::QTile q;
-            M::load_row(q, a.Q, row.at, r0 + col < rows, c.d, lane);
-            floatx4 sc[M::U];
-            M::scores(k, q, sc);
+    const int shift = __builtin_ctz(c.page), mask = c.page - 1;
+    constexpr int JUMP = SPLIT ? 64 : 16;  // rows of a turn
+    for (int w0 = first * ALL; w0 < s.kv; w0 += strides * ALL) {
+        const int t0 = w0 + (SPLIT ? 0 : wave * MINE);
+        typename M::KTile k[NK];
+        float w[NK][M::PER];
 #pragma unroll
-            for (int v = 0; v < M::PER; ++v) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(sc[v / 4][v % 4], c2, -row.lse2));
-                w[v] += t0 + M::key_of(g, v) < row.limit ? x : 0.f;
+        for (int m = 0; m < NK; ++m) {
+            const int from = t0 + m * KEYS;
+            M::load_k(c, k[m], page_of(c.table, c.width, c.pages, b, (from + M::k_group(lane)) >> shift),
+                      hk, from, lane);
+#pragma unroll
+            for (int v = 0; v < M::PER; ++v) w[m][v] = 0.f;
+        }
+        struct Stage {
+            typename M::QTile q;
+            float lse;
+            int limit;  // end of the keys that the row sees
+        };
+        auto load = [&](Stage& st, int r0) {
+            const bool live = r0 + col < rows;
+            const int r = live ? r0 + col : 0, i = int(group.quot(uint32_t(r))), h = hk * G + r - i * G;
+            st.lse = a.lse_in[int64_t(h) * a.tokens + s.q0 + i];
+            st.limit = !live ? 0 : a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+            M::load_row(st.q, a.Q, int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token, live, c.d,
+                        lane);
+        };
+        auto compute = [&](const Stage& st) {
+            const float neg = -st.lse * kLog2e;
+            const int limit = st.lse == -INFINITY ? 0 : st.limit;
+#pragma unroll
+            for (int m = 0; m < NK; ++m) {
+                floatx4 sc[M::U];
+                M::scores(k[m], st.q, sc);
+#pragma unroll
+                for (int v = 0; v < M::PER; ++v) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(sc[v / 4][v % 4], c2, neg));
+                    w[m][v] += t0 + m * KEYS + M::key_of(g, v) < limit ? x : 0.f;
+                }
+            }
+        };
+        // Rows before see none of these keys.
+        int r0 = a.causal ? max(0, t0 - (s.kv - s.n)) * G / 16 * 16 : 0;
+        if (SPLIT) r0 += 16 * wave;
+        if (r0 < rows) {
+            Stage A, B;
+            load(A, r0);
+            for (;;) {
+                if (r0 + JUMP < rows) load(B, r0 + JUMP);
+                compute(A);
+                r0 += JUMP;
+                if (r0 >= rows) break;
+                if (r0 + JUMP < rows) load(A, r0 + JUMP);
+                compute(B);
+                r0 += JUMP;
+                if (r0 >= rows) break;
             }
         }
-        float mine = 0.f;
+        __syncthreads();  // the sums before have been read
 #pragma unroll
-        for (int v = 0; v < M::PER; ++v) {
-            const float sum = group_sum(w[v]);
-            mine = v == col ? sum : mine;
-        }
-        const int key = t0 + M::key_of(g, col);
-        if (col < M::PER && key < s.kv) {
+        for (int m = 0; m < NK; ++m)
+#pragma unroll
+            for (int v = 0; v < M::PER; ++v) {
+                const float sum = group_sum(w[m][v]);
+                if (col == v) sums[wave][m * KEYS + M::key_of(g, v)] = sum;
+            }
+        __syncthreads();
+        const int mine = SPLIT ? int(threadIdx.x) : lane, key = t0 + mine;
+        if (mine < MINE && key < s.kv) {
+            float sum = sums[SPLIT ? 0 : wave][mine];
+            if (SPLIT)
+#pragma unroll
+                for (int o = 1; o < 4; ++o) sum += sums[o][mine];
             const int at = page_of(c.table, c.width, c.pages, b, key >> shift);
             if (at >= 0) {
-                float* to = c.weights + (int64_t(at) * c.H + hk) * c.page + (key & (c.page - 1));
-                *to = a.accumulate ? *to + mine : mine;
+                float* to = c.weights + (int64_t(at) * c.H + hk) * c.page + (key & mask);
+                *to = a.accumulate ? *to + sum : sum;
             }
         }
     }
+}
+
+template <typename T, int NK, bool SPLIT>
+hipError_t launch_keys(const PagedArgs& a, int most_kv, hipStream_t s) {
+    const int keys = (sizeof(T) == 2 ? 32 : 16) * NK * (SPLIT ? 1 : 4);
+    const int pairs = a.cache.B * a.cache.H;
+    const int strides = std::max(1, std::min((most_kv + keys - 1) / keys, (1 << 22) / pairs));
+    const Div group = make_div(uint32_t(a.q_heads / a.cache.H));
+    if (a.cache.d <= 64)
+        weights_keys_kernel<T, 64, NK, SPLIT><<<pairs * strides, 256, 0, s>>>(a, strides, group);
+    else
+        weights_keys_kernel<T, 128, NK, SPLIT><<<pairs * strides, 256, 0, s>>>(a, strides, group);
+    return hipGetLastError();
 }
 
 template <typename T, int NC>
@@ -225,14 +293,13 @@ hipError_t launch_paged_weights(const PagedArgs& a, hipStream_t s) {
         return bf16 ? launch_rows<uint16_t, 1>(a, most_kv, s) : launch_rows<float, 1>(a, most_kv, s);
     if (rows <= 32)
         return bf16 ? launch_rows<uint16_t, 2>(a, most_kv, s) : launch_rows<float, 2>(a, most_kv, s);
-    if (bf16) return launch_weights_tiles(a, s);
-    const int pairs = a.cache.B * a.cache.H;
-    const int strides = std::max(1, std::min((most_kv + 63) / 64, (1 << 22) / pairs));
-    if (a.cache.d <= 64)
-        weights_keys_kernel<float, 64><<<pairs * strides, 256, 0, s>>>(a, strides);
-    else
-        weights_keys_kernel<float, 128><<<pairs * strides, 256, 0, s>>>(a, strides);
-    return hipGetLastError();
+    // Workgroups of 64 keys.
+    const int64_t units = int64_t(a.cache.B) * a.cache.H * ((int64_t(most_kv) + 63) / 64);
+    if (bf16)
+        return units <= 2 * kCus ? launch_keys<uint16_t, 2, true>(a, most_kv, s)
+                                 : launch_weights_tiles(a, s);
+    return units < kCus || rows >= 2048 ? launch_keys<float, 1, true>(a, most_kv, s)
+                                        : launch_keys<float, 1, false>(a, most_kv, s);
 }
 
 }  // namespace sparsp

@@ -86,3 +86,24 @@ def test_no_new_tokens_writes_zero(gpu):
     R.close(w, bt.weights.double(), torch.zeros(1))
     sp.sparsp_paged_weights(q, torch.empty(2, 0, device="cuda"), weights=w, accumulate=False, **t)
     expect(bt, w, torch.empty(2, 0), None)
+
+
+@pytest.mark.parametrize("dtype,Hq,H,d,page,new,kv,bad",
+                         [c for c in CASES if sum(c[5]) * c[1] // c[2] > 32] +
+                         [(F, 4, 1, 8, 16, (600, 1, 0), (700, 30, 9), ((0, 3),)),
+                          (BF, 4, 1, 8, 16, (600, 1, 0), (700, 30, 9), ((0, 3),))])
+@pytest.mark.parametrize("causal", [True, False])
+def test_weights_of_a_wide_table(gpu, dtype, Hq, H, d, page, new, kv, bad, causal):
+    """Room for long sequences makes a launch of many workgroups, however short they are."""
+    bt = R.Batch(46, dtype, Hq, H, d, page, new, kv, tail=2, bad=bad, width=40000 // page)
+    lse = R.attention(bt, causal=causal)[1].float()
+    t, q = bt.to("cuda", "token")
+    del t["V_cache"]
+    w = bt.weights.cuda()
+    sp.sparsp_paged_weights(q, lse.cuda(), weights=w, causal=causal, **t)
+    expect(bt, w, lse, bt.weights, causal=causal)
+    # The same with the true lengths known, which few workgroups cover.
+    w = bt.weights.cuda()
+    sp.sparsp_paged_weights(q, lse.cuda(), weights=w, causal=causal, accumulate=False, max_kv=max(kv),
+                            max_new=max(new), **t)
+    expect(bt, w, lse, None, causal=causal)
