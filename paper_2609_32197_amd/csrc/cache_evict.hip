@@ -488,7 +488,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(const sparsp_cache c, in
     const int shift = __builtin_ctz(c.page), mask = c.page - 1;
     const int32_t* list = kept + int64_t(bh) * keep;
     // Three chunks at once, so that each waits once: the rows of this one are loaded beside the
-    // page numbers of the next one and the list of the one after (24 pairs of 2,900 to 6,007
+    // page numbers of the next one and the list of the one after (24 sequences of 2,900 to 6,007
     // tokens: 142 us with three waits for a chunk, 130 us).
     const int step = chunk_groups * chunk, row0 = int(threadIdx.x) >> lane_shift;
     int t[kDeep], p[kDeep], q[kDeep];
