@@ -13,8 +13,9 @@
 // Tiles are double-buffered: the copies of tile j+1 are issued right after the barrier that
 // opens tile j. They are direct-to-LDS buffer loads; a wave copies 16 rows, which lie on one
 // page, through a descriptor rooted at the first of them and ending with the sequence: rows
-// behind it, rows of a page that does not exist and channels behind d become zeros. The page numbers of the next 16,384 keys
-// are held in LDS, since a load of them in the loop would wait for the copies.
+// behind it, rows of a page that does not exist and channels behind d become zeros. The page
+// numbers of the next 16,384 keys are held in LDS, since a load of them in the loop would wait
+// for the copies.
 //
 // Swizzle: 16-byte chunks of an LDS row are exchanged by an XOR with bits of the row, applied to
 // the source addresses of the copies. K rows read together by 16 lanes (8 i + j + const,

@@ -179,8 +179,9 @@ __global__ __launch_bounds__(256) void weights_keys_kernel(const PagedArgs a, in
 #pragma unroll
         for (int m = 0; m < NK; ++m) {
             const int from = t0 + m * KEYS;
-            M::load_k(c, k[m], page_of(c.table, c.width, c.pages, b, (from + M::k_group(lane)) >> shift),
-                      hk, from, lane);
+            const int page =
+                page_of(c.table, c.width, c.pages, b, (from + M::k_group(lane)) >> shift);
+            M::load_k(c, k[m], page, hk, from, lane);
 #pragma unroll
             for (int v = 0; v < M::PER; ++v) w[m][v] = 0.f;
         }
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(256) void weights_keys_kernel(const PagedArgs a, in
         };
         auto load = [&](Stage& st, int r0) {
             const bool live = r0 + col < rows;
-            const int r = live ? r0 + col : 0, i = int(group.quot(uint32_t(r))), h = hk * G + r - i * G;
+            const int r = live ? r0 + col : 0, i = int(group.quot(uint32_t(r)));
+            const int h = hk * G + r - i * G;
             st.lse = a.lse_in[int64_t(h) * a.tokens + s.q0 + i];
             st.limit = !live ? 0 : a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
             M::load_row(st.q, a.Q, int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token, live, c.d,

@@ -74,8 +74,9 @@ __device__ __forceinline__ void put(Vec<T, V>* p, Vec<T, V> x, bool stream) {
 }
 
 // A workgroup's places: for each token the byte offset of its row in the pages, kNoPlace, or
-// kNoSequence for a column of no sequence, which nothing is written for. A wave takes a token: new_off is ascending, so the token's sequence is the number of ends
-// new_off[1..B] at or before it, counted 64 at a time.
+// kNoSequence for a column of no sequence, which nothing is written for. A wave takes a token:
+// new_off is ascending, so the token's sequence is the number of ends new_off[1..B] at or before
+// it, counted 64 at a time.
 constexpr int64_t kNoPlace = -1, kNoSequence = -2;
 template <typename T>
 __device__ __forceinline__ void find_places(const Params& p, int t0, int count, int64_t* place) {

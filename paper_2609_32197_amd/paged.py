@@ -206,8 +206,9 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
                 inverse: bool = False, stream=None):
     """X [heads, tokens, d] rotated to positions [axes, tokens] (or [tokens]); X2 alike.
 
-    Returns Y (in X's order of heads and tokens, unless given), or (Y, Y2) with X2. Y may be X (in place). With inverse the transposed rotation:
-    it turns back (times factor squared), and carries a gradient of Y to one of X.
+    Returns Y (in X's order of heads and tokens, unless given), or (Y, Y2) with X2. Y may be X (in
+    place). With inverse the transposed rotation: it turns back (times factor squared), and
+    carries a gradient of Y to one of X.
     """
     torch = _torch()
     if not isinstance(X, torch.Tensor):
@@ -217,7 +218,8 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
         raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
     dev, (_, n, d) = X.get_device(), X.shape
     y = Y if Y is not None else torch.empty_like(X)
-    x, o, count = _rows(X, "X", dev, X.dtype, n, d), _rows(y, "Y", dev, X.dtype, n, d, X.shape[0]), 1
+    x, count = _rows(X, "X", dev, X.dtype, n, d), 1
+    o = _rows(y, "Y", dev, X.dtype, n, d, X.shape[0])
     y2 = None
     if X2 is not None:
         x += _rows(X2, "X2", dev, X.dtype, n, d)
@@ -227,8 +229,8 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     elif Y2 is not None:
         raise ValueError("Y2 needs X2")
     pos, bits, freq = _positions(rotary, positions, inv_freq, n, dev)
-    _call(load_library().sparsp_rope, dev, stream, rotary._pack(inverse), n, d, code, x, o, count, pos, bits,
-            freq)
+    _call(load_library().sparsp_rope, dev, stream, rotary._pack(inverse), n, d, code, x, o, count,
+          pos, bits, freq)
     return y if X2 is None else (y, y2)
 
 
@@ -257,7 +259,7 @@ def _cache(K_cache, V_cache, weights, page_table, new_off, kv_len):
 def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, weights=None,
                         rotary: Optional[Rotary] = None, positions=None, inv_freq=None, Q=None,
                         Q_out=None, stream=None):
-    """Writes the new tokens' K, V [H, tokens, d] into the cache (and 0 into their weights, if given).
+    """Writes the new tokens' K, V [H, tokens, d] into the cache (and 0 into weights, if given).
 
     With a rotation K is rotated to its positions on the way, and so is Q, into Q_out (which may
     be Q). Returns Q_out, or None without Q.
@@ -278,7 +280,7 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
     elif Q_out is not None:
         raise ValueError("Q_out needs Q")
     _call(load_library().sparsp_paged_append, dev, stream, c, n, _rows(K, "K", dev, dt, n, d, H),
-            _rows(V, "V", dev, dt, n, d, H), rot, pos, bits, freq, q, qo)
+          _rows(V, "V", dev, dt, n, d, H), rot, pos, bits, freq, q, qo)
     return Q_out
 
 
@@ -327,9 +329,9 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
         ws = _on(workspace, "workspace", dev)
         nbytes = workspace.numel() * workspace.element_size()
     _call(load_library().sparsp_paged_attn, dev, stream, c, n, _rows(Q, "Q", dev, dt, n, d),
-            _rows(o, "O", dev, odt, n, d, heads), int(out_dtype),
-            None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
-            bool(causal), _scale(softmax_scale, d), int(max_new or 0), int(max_kv or 0), ws, nbytes)
+          _rows(o, "O", dev, odt, n, d, heads), int(out_dtype),
+          None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
+          bool(causal), _scale(softmax_scale, d), int(max_new or 0), int(max_kv or 0), ws, nbytes)
     return o, ls
 
 
@@ -351,9 +353,10 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
         raise ValueError(f"Q must have d = {K_cache.shape[3]} (got {d})")
     if weights is None:
         raise TypeError("weights must be a torch.Tensor")
-    _call(load_library().sparsp_paged_weights, dev, stream, c, n, _rows(Q, "Q", dev, K_cache.dtype, n, d),
-            _on(lse, "lse", dev, torch.float32, (heads, n)) or 16, bool(causal),
-            _scale(softmax_scale, d), bool(accumulate), int(max_new or 0), int(max_kv or 0))
+    _call(load_library().sparsp_paged_weights, dev, stream, c, n,
+          _rows(Q, "Q", dev, K_cache.dtype, n, d),
+          _on(lse, "lse", dev, torch.float32, (heads, n)) or 16, bool(causal),
+          _scale(softmax_scale, d), bool(accumulate), int(max_new or 0), int(max_kv or 0))
     return weights
 
 
