@@ -90,13 +90,16 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             typename M::VTile v;
             int kp, vp;
         };
-        auto load = [&](Stage& st, int t0, int p0) {
+        auto load_k = [&](Stage& st, int t0, int p0) {
             st.kp = page_list[((t0 + M::k_group(lane)) >> shift) - p0];
-            st.vp = page_list[((t0 + M::v_group(lane)) >> shift) - p0];
             M::load_k(c, st.k, st.kp, hk, t0, lane);
+        };
+        auto load_v = [&](Stage& st, int t0, int p0) {
+            st.vp = page_list[((t0 + M::v_group(lane)) >> shift) - p0];
             M::load_v(c, st.v, st.vp, hk, t0, lane);
         };
-        auto compute = [&](Stage& st, int t0) {
+        // after_scores: what is done once K has been used.
+        auto compute = [&](Stage& st, int t0, auto after_scores) {
             const bool masked =
                 __ballot(t0 + KEYS > lowest || t0 + KEYS > end || st.kp < 0 || st.vp < 0) != 0;
             if (masked) {
@@ -106,13 +109,15 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
                 M::clear_v(st.v, live);
             }
             typename M::P pr[NC];
+            floatx4 sc[NC][M::U];
+#pragma unroll
+            for (int n = 0; n < NC; ++n) M::scores(st.k, q[n], sc[n]);
+            after_scores();
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
-                floatx4 sc[M::U];
-                M::scores(st.k, q[n], sc);
                 float p[M::PER];
 #pragma unroll
-                for (int v = 0; v < M::PER; ++v) p[v] = sc[v / 4][v % 4];
+                for (int v = 0; v < M::PER; ++v) p[v] = sc[n][v / 4][v % 4];
                 if (masked) {
                     const int lim = st.vp < 0 ? 0 : min(limit[n], part_end);
 #pragma unroll
@@ -144,9 +149,9 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
         };
 
         // Two tiles in flight: one is computed while the next is loaded. (With 32 rows the
-        // registers hold one tile; the CU's other waves cover its loads.) The page numbers of
-        // the next 16,384 keys lie in LDS: a load of them would return in order with the rows
-        // asked for before.
+        // registers hold one tile: the next one's K is loaded once the scores are there, its V
+        // behind the output.) The page numbers of the next 16,384 keys lie in LDS: a load of
+        // them would return in order with the rows asked for before.
         constexpr int JUMP = 4 * KEYS;
         for (int seg = lo; seg < end; seg += kSegment) {
             const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
@@ -158,28 +163,34 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             int t0 = seg + wave * KEYS;
             if (t0 >= seg_end) continue;
             Stage A;
-            load(A, t0, p0);
-            auto next = [&](Stage& st) {
-                if (t0 + JUMP < seg_end) load(st, t0 + JUMP, p0);
-            };
+            load_k(A, t0, p0);
+            load_v(A, t0, p0);
             if constexpr (NC == 1) {
                 Stage B;
+                auto next = [&](Stage& st) {
+                    if (t0 + JUMP >= seg_end) return;
+                    load_k(st, t0 + JUMP, p0);
+                    load_v(st, t0 + JUMP, p0);
+                };
                 for (;;) {
                     next(B);
-                    compute(A, t0);
+                    compute(A, t0, [] {});
                     t0 += JUMP;
                     if (t0 >= seg_end) break;
                     next(A);
-                    compute(B, t0);
+                    compute(B, t0, [] {});
                     t0 += JUMP;
                     if (t0 >= seg_end) break;
                 }
             } else {
                 for (;;) {
-                    compute(A, t0);
-                    next(A);
+                    const bool more = t0 + JUMP < seg_end;
+                    compute(A, t0, [&] {
+                        if (more) load_k(A, t0 + JUMP, p0);
+                    });
+                    if (!more) break;
                     t0 += JUMP;
-                    if (t0 >= seg_end) break;
+                    load_v(A, t0, p0);
                 }
             }
         }
