@@ -36,15 +36,10 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     const sparsp_cache& c = a.cache;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, g = lane >> 4;
-    // The row tiles of one part of the keys run on one XCD, one after another, so that all
-    // but the first find the keys in its L2.
-    const int units = c.B * c.H * plan.parts;
-    const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
-    const int unit = k / plan.tiles * 8 + xcd;
-    if (unit >= units) return;
-    const auto [bh, part] = unit_of(unit, c.B * c.H);
-    const int b = bh / c.H, hk = bh % c.H;
     const int G = a.q_heads / c.H;
+    Work work;
+    if (!work_of<16 * NC>(plan, c, a.tokens, G, &work)) return;
+    const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
     const int keys = part_keys(plan, s.kv);
@@ -54,7 +49,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     const float c2 = a.scale * kLog2e;
     const int shift = __builtin_ctz(c.page);
 
-    for (int tile = k % plan.tiles; tile * int64_t(16 * NC) < rows; tile += plan.tiles) {
+    for (int tile = work.tile; tile * int64_t(16 * NC) < rows; tile += work.stride) {
         typename M::QTile q[NC];
         int limit[NC], lowest = 1 << 30;  // keys before limit are seen
         int end = 0;
@@ -369,12 +364,17 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / std::max<int64_t>(pairs, 8));
     tiles = std::min(tiles, room);
     const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
-    const int64_t rounds = (int64_t(most_kv) + round - 1) / round, units = pairs * tiles;
+    const int64_t rounds = (int64_t(most_kv) + round - 1) / round;
+    // Row tiles that can have work. With one long sequence among many they are few of pairs *
+    // tiles, whose workgroups, most of them empty, would cost more than finding a workgroup's
+    // tile (32 heads of 128, 256 sequences of one new token and one of 1,024 over 2,000 each: 900
+    // us, 386 us; the two kinds by themselves: 356 and 58 us).
+    const int64_t flat = a.tokens * int64_t(G) / r.rows + c.B;
+    const int64_t live = std::min(pairs * tiles, c.H * flat);
+    if (pairs * tiles > 2 * live) r.plan.flat = int(flat);
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
-    if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, units * parts / 128) : 0)) parts = 1;
-    if (units * parts > 2 * kCus) {
-        // (of the tiles of the longest sequence, those that all the new tokens can fill)
-        const int64_t live = std::min(units, c.H * (a.tokens * int64_t(G) / r.rows + c.B));
+    if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, live * parts / 128) : 0)) parts = 1;
+    if (live * parts > 2 * kCus) {
         int64_t fill = 2 * kCus / std::min<int64_t>(live, 2 * kCus);
         if (rounds >= 16 && live < 2 * kCus && live * fill < 3 * kCus / 2) fill *= 4;
         const int64_t level = 16 * kCus / std::min<int64_t>(live, 16 * kCus);
@@ -395,8 +395,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
 
 template <typename T, int D, int NC>
 hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
-    const int units = (a.cache.B * a.cache.H * p.parts + 7) / 8 * 8;
-    paged_rows_kernel<T, D, NC><<<units * p.tiles, 256, 0, s>>>(a, p);
+    paged_rows_kernel<T, D, NC><<<workgroups(p, a.cache), 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
@@ -430,7 +429,7 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
     const int64_t pairs = int64_t(a.cache.B) * a.q_heads;
     const bool shared = pairs * most_new <= 16 * kCus;
     const int64_t runs = shared ? most_new : (most_new + 7) / 8;  // workgroups of a head
-    const int per = int(std::min(runs, std::max<int64_t>(1, (int64_t(1) << 22) / pairs)));
+    const int per = int(std::min(runs, std::max<int64_t>(1, (int64_t(1) << 15) / pairs)));
     if (shared)
         paged_merge_kernel<true><<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
     else

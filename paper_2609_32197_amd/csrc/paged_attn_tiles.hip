@@ -123,14 +123,10 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    // The row tiles of one part of the keys run on one XCD, one after another.
-    const int units = c.B * c.H * plan.parts;
-    const int turn = blockIdx.x >> 3;
-    const int unit = turn / plan.tiles * 8 + (blockIdx.x & 7);
-    if (unit >= units) return;
-    const auto [bh, part] = unit_of(unit, c.B * c.H);
-    const int b = bh / c.H, hk = bh % c.H;
     const int G = a.q_heads / c.H;
+    Work work;
+    if (!work_of<kRowsTile>(plan, c, a.tokens, G, &work)) return;
+    const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
     const int keys = part_keys(plan, s.kv);
@@ -167,7 +163,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                                    (col & 1) * 8);
 
     // Later row tiles see more keys: they come first.
-    for (int turns = turn % plan.tiles; turns * int64_t(kRowsTile) < rows; turns += plan.tiles) {
+    for (int turns = work.tile; turns * int64_t(kRowsTile) < rows; turns += work.stride) {
         const int n_tiles = (rows + kRowsTile - 1) / kRowsTile;
         const int tile = n_tiles - 1 - turns;
         bf16x8 q[2][KT];
@@ -401,13 +397,13 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
 }  // namespace
 
 hipError_t launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
-    const int units = (a.cache.B * a.cache.H * p.parts + 7) / 8 * 8;
+    const int grid = workgroups(p, a.cache);
     if (a.cache.d <= 64)
-        paged_tiles_kernel<64, 64><<<units * p.tiles, 256, 0, s>>>(a, p);
+        paged_tiles_kernel<64, 64><<<grid, 256, 0, s>>>(a, p);
     else if (a.cache.d <= 96)
-        paged_tiles_kernel<128, 96><<<units * p.tiles, 256, 0, s>>>(a, p);
+        paged_tiles_kernel<128, 96><<<grid, 256, 0, s>>>(a, p);
     else
-        paged_tiles_kernel<128, 128><<<units * p.tiles, 256, 0, s>>>(a, p);
+        paged_tiles_kernel<128, 128><<<grid, 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 

@@ -6,9 +6,10 @@
 
 namespace sparsp {
 
-// `tiles` workgroups stride over a sequence's row tiles, `parts` over its keys.
+// `tiles` workgroups stride over a sequence's row tiles, `parts` over its keys. With `flat` row
+// tiles of all sequences at most, a workgroup finds its own among them instead.
 struct PagedPlan {
-    int tiles, parts, step;
+    int tiles, parts, step, flat;
     float* part_o;    // [q_heads, tokens, parts, d]
     float* part_lse;  // [q_heads, tokens, parts]
 };
@@ -31,6 +32,61 @@ struct Unit {
 __device__ __forceinline__ Unit unit_of(int u, int pairs) {
     const int part = u / pairs;
     return {(u % pairs + pairs - part % pairs) % pairs, part};
+}
+
+// What a workgroup does: the row tiles tile, tile + stride, ... of a sequence and key head, and a
+// part of the keys.
+struct Work {
+    int b, hk, part, tile, stride;
+};
+// Row tile number f of all sequences' tiles of ROWS rows. Each wave counts the tiles of 64
+// sequences at a time.
+template <int ROWS>
+__device__ __forceinline__ bool find_tile(const sparsp_cache& c, int tokens, int G, int f, Work* w) {
+    const int lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64) {
+        const int n = b0 + lane < c.B ? sequence(c, tokens, b0 + lane).n : 0;
+        const uint32_t mine = uint32_t(n * G + ROWS - 1) / ROWS;
+        uint32_t sum = mine;  // (exact up to the first lane that passes f, whatever new_off holds)
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const uint32_t y = __shfl_up(sum, off);
+            if (lane >= off) sum += y;
+        }
+        const uint64_t behind = __ballot(before + sum > uint32_t(f));
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            w->b = b0 + l;
+            w->tile = f - int(before) - int(__builtin_amdgcn_readlane(sum - mine, l));
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+// False: nothing. The row tiles of one part of the keys run on one XCD, one after another, so
+// that all but the first find the keys in its L2; of flat tiles, eight in a row.
+template <int ROWS>
+__device__ __forceinline__ bool work_of(const PagedPlan& p, const sparsp_cache& c, int tokens, int G,
+                                        Work* w) {
+    const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
+    if (p.flat) {
+        const int item = ((k >> 3) * 8 + xcd) * 8 + (k & 7), unit = item / p.flat;
+        w->hk = unit % c.H;
+        w->part = unit / c.H;
+        w->stride = 1 << 30;
+        return w->part < p.parts && find_tile<ROWS>(c, tokens, G, item % p.flat, w);
+    }
+    const int unit = k / p.tiles * 8 + xcd;
+    if (unit >= c.B * c.H * p.parts) return false;
+    const auto [bh, part] = unit_of(unit, c.B * c.H);
+    *w = {bh / c.H, bh % c.H, part, k % p.tiles, p.tiles};
+    return true;
+}
+inline int workgroups(const PagedPlan& p, const sparsp_cache& c) {
+    return p.flat ? (p.flat * c.H * p.parts + 63) / 64 * 64
+                  : (c.B * c.H * p.parts + 7) / 8 * 8 * p.tiles;
 }
 
 // Keys of a part of a sequence of kv cached tokens: a multiple of step, so many that

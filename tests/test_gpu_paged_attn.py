@@ -250,3 +250,14 @@ def test_more_row_tiles_than_a_grid_holds(gpu):
     tO = A * (4 * e[..., None] + 2 * (kv + 64) * R.U + 2.0 ** -18) + R.U * w.abs()
     R.close(O[:, at], w, tO, "O")
     assert torch.isfinite(O).all()
+
+
+@pytest.mark.parametrize("dtype,Hq,H,d", [(BF, 4, 2, 128), (BF, 3, 1, 80), (BF, 6, 1, 64), (F, 4, 1, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_prompts_among_many_single_tokens(gpu, dtype, Hq, H, d, causal):
+    """More than 64 sequences, of which two have many tokens and some none."""
+    new = (1, 0, 1, 5, 300) + (1,) * 60 + (0, 0, 417, 2, 1, 0)
+    kv = tuple(n if b % 7 == 1 else n + 40 * (b % 5) + 900 * (b % 23 == 4) for b, n in enumerate(new))
+    bt = R.Batch(33, dtype, Hq, H, d, 16, new, kv, tail=3, bad=((4, 2),))
+    for ws, hint in ((True, True), (False, True), (True, False)):
+        check(bt, *run(bt, "token", ws, causal=causal, hint=hint), causal=causal)
