@@ -305,10 +305,11 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 }
                 // The reference of a row's exponentials moves only where they grow past it: where a
                 // lane's eight sum to more than 2^8, or the row has seen nothing yet. A sum of
-                // positive numbers bounds them all, so the other tiles take no maximum (48
-                // heads of d = 64, prompts of 902 to 4,095 tokens: 290 us with one in every tile, 271
-                // us without; d = 128, chunks of 2,048 over 32,768: 1,653 and 1,601 us). A probability is rounded to bf16 by
-                // the same share of itself wherever the reference lies.
+                // positive numbers bounds them all, so the other tiles take no maximum (48 heads of
+                // d = 64, prompts of 902 to 4,095 tokens: 290 us with one in every tile, 271 us
+                // without; d = 128, chunks of 2,048 over 32,768: 1,653 and 1,601 us). A
+                // probability is rounded to bf16 by the same share of itself wherever the
+                // reference lies.
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     floatx8 p[2];
