@@ -197,10 +197,9 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
         const int end = min(a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv, part_end);
 
         floatx4 acc[2][DT];
-        float m[2], l[2], lim[2], base[2];  // reference (log2 units), mass, see below
+        float l[2], lim[2], base[2];  // mass, see below, minus the reference (log2 units)
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-            m[n] = -INFINITY;
             lim[n] = limit[n] > 0 ? -1.f : INFINITY;  // (a row that sees nothing never asks)
             l[n] = base[n] = 0.f;
 #pragma unroll
@@ -331,10 +330,10 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                             float mx = -INFINITY;
 #pragma unroll
                             for (int v = 0; v < 8; ++v) mx = fmaxf(mx, sc[n][2 * t + v / 4][v % 4]);
-                            const float top = fmaxf(m[n], quad_max(mx) * c2);
+                            const float before = lim[n] == 256.f ? -base[n] : -INFINITY;
+                            const float top = fmaxf(before, quad_max(mx) * c2);
                             const float alpha =
-                                top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
-                            m[n] = top;
+                                top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(before - top);
                             l[n] *= alpha;
                             lim[n] = top > -INFINITY ? 256.f : limit[n] > 0 ? -1.f : INFINITY;
                             base[n] = top == -INFINITY ? 0.f : -top;
@@ -377,7 +376,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
             const int i = r / G, h = hk * G + r % G;
             const bool any = total > 0.f;
             const float inv = any ? 1.f / total : 0.f;
-            const float lse = any ? (m[n] + __log2f(total)) * kLn2 : -INFINITY;
+            const float lse = any ? (__log2f(total) - base[n]) * kLn2 : -INFINITY;
             const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
             const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
                                      : (at * plan.parts + part) * c.d;
