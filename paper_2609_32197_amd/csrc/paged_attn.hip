@@ -340,9 +340,11 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
 // that a ragged batch fills the GPU to the end: 64 sequences of 400 to 9,001 tokens, 4 rows each,
 // take 195 us whole and 140 us in 5 parts, with 40 rows 221 us in one and 162 us in 5 (32 of
 // 8,000 each, which gain nothing by it, 192 and 198 us); float32, 710 to 279 tokens of 5
-// sequences over 5,671 to 9,606: 1,330 us whole, 984 us. bf16 rows of more than 64 do not gain
-// (128 each: 229 us either way; 32 of 8,000: 209 us in 2 parts, 243 us in 4). There are no more
-// parts than the workspace holds.
+// sequences over 5,671 to 9,606: 1,330 us whole, 984 us. bf16 rows of more than 64, whose partial
+// rows cost more, take parts of 32 rounds where their workgroups are two a CU at most and that
+// is twice as many parts (16 heads of 64, 796 and 284 tokens over 45,429 and 12,913: 365 us in 3
+// parts, 231 us in 12; 84 heads of 128, 109 to 55 over 10,471 to 2,812: 168 us in 2, 189 us in
+// 3). There are no more parts than the workspace holds.
 struct Shape {
     PagedPlan plan;
     int rows;       // of a tile
@@ -378,10 +380,10 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
         int64_t fill = 2 * kCus / std::min<int64_t>(live, 2 * kCus);
         if (rounds >= 16 && live < 2 * kCus && live * fill < 3 * kCus / 2) fill *= 4;
         const int64_t level = 16 * kCus / std::min<int64_t>(live, 16 * kCus);
-        const int64_t least = c.dtype == SPARSP_F32 ? 8 : 16;  // rounds of a part
-        parts = r.rows == 128 && rows > 64
-                    ? fill
-                    : std::max(fill, std::min(level, (rounds + least - 1) / least));
+        const bool tall = r.rows == 128 && rows > 64;
+        const int64_t least = c.dtype == SPARSP_F32 ? 8 : tall ? 32 : 16;  // rounds of a part
+        parts = std::max(fill, std::min(level, (rounds + least - 1) / least));
+        if (tall && (live > 2 * kCus || parts < 2 * fill)) parts = fill;
         parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
     }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
