@@ -367,13 +367,9 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     tiles = std::min(tiles, room);
     const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
     const int64_t rounds = (int64_t(most_kv) + round - 1) / round;
-    // Row tiles that can have work. With one long sequence among many they are few of pairs *
-    // tiles, whose workgroups, most of them empty, would cost more than finding a workgroup's
-    // tile (32 heads of 128, 256 sequences of one new token and one of 1,024 over 2,000 each: 900
-    // us, 386 us; the two kinds by themselves: 356 and 58 us).
+    // Row tiles that can have work.
     const int64_t flat = a.tokens * int64_t(G) / r.rows + c.B;
     const int64_t live = std::min(pairs * tiles, c.H * flat);
-    if (pairs * tiles > 2 * live) r.plan.flat = int(flat);
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
     if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, live * parts / 128) : 0)) parts = 1;
     if (live * parts > 2 * kCus) {
@@ -388,6 +384,17 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     }
     const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
+    // Each workgroup finds its tile among those that have work, where they are few of pairs *
+    // tiles: one long sequence among many, whose empty workgroups would cost more (32 heads of
+    // 128, 256 sequences of one new token and one of 1,024 over 2,000 each: 900 us, 386 us; the
+    // two kinds by themselves: 356 and 58 us). And where key heads leave XCDs less to do than
+    // others (2 of 128, 2,000 tokens over 6,000: 203 us, 110 us; 5 of 64: 187 and 138 us; 4
+    // sequences of 806 to 2,000 tokens, 2 heads: 184 and 115 us), but not like sequences that
+    // fill all eight (4 of 2,000 tokens, 2 heads: 53 and 60 us).
+    const bool even = a.tokens == int64_t(c.B) * most_new && parts == 1 && pairs % 8 == 0;
+    if (pairs * tiles > 2 * live || (tiles >= 8 && c.H % 8 != 0 && pairs * parts < 64 && !even &&
+                                     c.H * flat * parts <= 1 << 20))
+        r.plan.flat = int(flat);
     r.plan.step = int((rounds + parts - 1) / parts) * round;
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);

@@ -66,17 +66,21 @@ __device__ __forceinline__ bool find_tile(const sparsp_cache& c, int tokens, int
     return false;
 }
 // False: nothing. The row tiles of one part of the keys run on one XCD, one after another, so
-// that all but the first find the keys in its L2; of flat tiles, eight in a row.
+// that all but the first find the keys in its L2. Flat tiles do so eight at a time, all heads'
+// and parts' first eight before the next, and with parts, of which the later ones have less to
+// do, the next eight on another XCD.
 template <int ROWS>
 __device__ __forceinline__ bool work_of(const PagedPlan& p, const sparsp_cache& c, int tokens, int G,
                                         Work* w) {
     const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
     if (p.flat) {
-        const int item = ((k >> 3) * 8 + xcd) * 8 + (k & 7), unit = item / p.flat;
+        const int turn = (k >> 3) * 8 + xcd, units = c.H * p.parts;
+        const int run = turn / units, f = run * 8 + (k & 7);
+        const int unit = (turn + (p.parts > 1 ? run : 0)) % units;
         w->hk = unit % c.H;
         w->part = unit / c.H;
         w->stride = 1 << 30;
-        return w->part < p.parts && find_tile<ROWS>(c, tokens, G, item % p.flat, w);
+        return f < p.flat && find_tile<ROWS>(c, tokens, G, f, w);
     }
     const int unit = k / p.tiles * 8 + xcd;
     if (unit >= c.B * c.H * p.parts) return false;
@@ -85,7 +89,7 @@ __device__ __forceinline__ bool work_of(const PagedPlan& p, const sparsp_cache& 
     return true;
 }
 inline int workgroups(const PagedPlan& p, const sparsp_cache& c) {
-    return p.flat ? (p.flat * c.H * p.parts + 63) / 64 * 64
+    return p.flat ? ((p.flat + 7) / 8 * c.H * p.parts + 7) / 8 * 64
                   : (c.B * c.H * p.parts + 7) / 8 * 8 * p.tiles;
 }
 
