@@ -196,8 +196,12 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
         const int last = min(rows, (tile + 1) * kRowsTile) - 1;
         const int end = min(a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv, part_end);
 
+        // l: sum of exponentials. lim: what a lane's eight may sum to before the reference moves;
+        // kSeen, or -1: the row has seen nothing yet, or kFar. base: minus the reference in log2
+        // units, or with kFar the reference as a score.
+        constexpr float kSeen = 256.f, kFar = -2.f;
         floatx4 acc[2][DT];
-        float l[2], lim[2], base[2];  // mass, see below, minus the reference (log2 units)
+        float l[2], lim[2], base[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             lim[n] = limit[n] > 0 ? -1.f : INFINITY;  // (a row that sees nothing never asks)
@@ -313,14 +317,17 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 for (int t = 0; t < 2; ++t) {
                     floatx8 p[2];
                     float sum[2];
+                    auto add = [&](int n) {
+                        sum[n] = p[n][0];
+#pragma unroll
+                        for (int v = 1; v < 8; ++v) sum[n] += p[n][v];
+                    };
                     auto exponentials = [&](int n) {
 #pragma unroll
                         for (int v = 0; v < 8; ++v)
                             p[n][v] = __builtin_amdgcn_exp2f(
                                 fmaf(sc[n][2 * t + v / 4][v % 4], c2, base[n]));
-                        sum[n] = p[n][0];
-#pragma unroll
-                        for (int v = 1; v < 8; ++v) sum[n] += p[n][v];
+                        add(n);
                     };
                     exponentials(0);
                     exponentials(1);
@@ -330,16 +337,33 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                             float mx = -INFINITY;
 #pragma unroll
                             for (int v = 0; v < 8; ++v) mx = fmaxf(mx, sc[n][2 * t + v / 4][v % 4]);
-                            const float before = lim[n] == 256.f ? -base[n] : -INFINITY;
-                            const float top = fmaxf(before, quad_max(mx) * c2);
-                            const float alpha =
-                                top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(before - top);
+                            mx = quad_max(mx);
+                            // A reference of 2^24 and more in log2 units is rounded by a half and
+                            // more, one of 2^32 by more than an exponential can make good. Such a
+                            // row keeps its reference as a score and subtracts that first, in this
+                            // branch, into which its limit sends every tile from then on.
+                            const bool was_far = lim[n] == kFar;
+                            const float before = lim[n] == kSeen ? -base[n] : -INFINITY;
+                            const float top = fmaxf(before, mx * c2);
+                            const bool far =
+                                was_far || (mx > -INFINITY && !(fabsf(top) < 0x1p24f));
+                            const float ref = was_far ? fmaxf(base[n], mx) : mx;
+                            float alpha = far ? fmaf(-ref, c2, before) : before - top;
+                            if (was_far) alpha = (base[n] - ref) * c2;
+                            alpha = !far && top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(alpha);
                             l[n] *= alpha;
-                            lim[n] = top > -INFINITY ? 256.f : limit[n] > 0 ? -1.f : INFINITY;
-                            base[n] = top == -INFINITY ? 0.f : -top;
+                            lim[n] = far ? kFar
+                                     : top > -INFINITY ? kSeen : limit[n] > 0 ? -1.f : INFINITY;
+                            base[n] = far ? ref : top == -INFINITY ? 0.f : -top;
 #pragma unroll
                             for (int dt = 0; dt < DT; ++dt) acc[n][dt] *= alpha;
-                            exponentials(n);
+#pragma unroll
+                            for (int v = 0; v < 8; ++v) {
+                                const float x = sc[n][2 * t + v / 4][v % 4];
+                                p[n][v] = __builtin_amdgcn_exp2f(far ? (x - base[n]) * c2
+                                                                     : fmaf(x, c2, base[n]));
+                            }
+                            add(n);
                         }
                     }
                     bf16x8 pb[2];
@@ -376,7 +400,9 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
             const int i = r / G, h = hk * G + r % G;
             const bool any = total > 0.f;
             const float inv = any ? 1.f / total : 0.f;
-            const float lse = any ? (__log2f(total) - base[n]) * kLn2 : -INFINITY;
+            const float lse = !any ? -INFINITY
+                              : lim[n] == kFar ? fmaf(base[n], a.scale, __logf(total))
+                                               : (__log2f(total) - base[n]) * kLn2;
             const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
             const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
                                      : (at * plan.parts + part) * c.d;
