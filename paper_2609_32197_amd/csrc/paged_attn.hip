@@ -12,8 +12,8 @@
 // to paged_attn_tiles.hip.
 //
 // Long caches are split: each part (a multiple of `step` keys) writes its normalised
-// output and lse, float32, to the workspace, and a merge kernel joins a row's parts in
-// their order. A sequence short enough for one part writes its output directly.
+// output, its sum of exponentials and the score they are relative to, float32, to the workspace,
+// and a merge kernel joins a row's parts in their order. A sequence short enough for one part writes its output directly.
 #include <algorithm>
 #include <cmath>
 
@@ -224,16 +224,19 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
                 const float inv = any ? 1.f / total : 0.f;
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] * inv : 0.f;
-                const float lse = any ? fmaf(top, a.scale, __logf(total)) : -INFINITY;
                 const int i = r / G, h = hk * G + r % G;
                 const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
                 if (whole) {
                     store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch,
                            a.out_bf16, x);
-                    if (ch == 0 && a.lse) a.lse[at] = lse;
+                    if (ch == 0 && a.lse)
+                        a.lse[at] = any ? fmaf(top, a.scale, __logf(total)) : -INFINITY;
                 } else {
                     store4(plan.part_o, (at * plan.parts + part) * c.d + ch, false, x);
-                    if (ch == 0) plan.part_lse[at * plan.parts + part] = lse;
+                    if (ch == 0) {
+                        plan.part_sum[at * plan.parts + part] = total;
+                        plan.part_ref[at * plan.parts + part] = top;
+                    }
                 }
             }
         }
@@ -256,15 +259,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     const int keys = part_keys(plan, s.kv);
     if (s.kv <= keys) return;
     const int parts = (s.kv + keys - 1) / keys;
+    const float c2 = a.scale * kLog2e;
     const int group = threadIdx.x >> 5, lane = threadIdx.x & 31, ch = lane * 4;
     const int first = SHARED ? group : 0, stride = SHARED ? 8 : 1;  // of a group's parts
     constexpr int ROWS = SHARED ? 1 : 8, DEEP = 4;                  // DEEP parts in flight
     for (int i0 = blockIdx.x % per_head * ROWS; i0 < s.n; i0 += per_head * ROWS) {
         const int i = SHARED ? i0 : min(i0 + group, s.n - 1);
         const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
-        const float* lse = plan.part_lse + at * plan.parts;
+        const float *sum = plan.part_sum + at * plan.parts, *ref = plan.part_ref + at * plan.parts;
         float top = -INFINITY;
-        for (int p = lane; p < parts; p += 32) top = fmaxf(top, lse[p]);
+        for (int p = lane; p < parts; p += 32) top = fmaxf(top, ref[p]);
 #pragma unroll
         for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
         const float base = top == -INFINITY ? 0.f : top;
@@ -272,17 +276,18 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
         const float* from = plan.part_o + at * plan.parts * c.d + (ch < c.d ? ch : 0);
         for (int p0 = first; p0 < parts; p0 += stride * DEEP) {
             floatx4 y[DEEP];
-            float part[DEEP];
+            float part[DEEP], mass[DEEP];
 #pragma unroll
             for (int u = 0; u < DEEP; ++u) {
                 const int p = min(p0 + stride * u, parts - 1);
                 y[u] = *reinterpret_cast<const floatx4*>(from + int64_t(p) * c.d);
-                part[u] = lse[p];
+                part[u] = ref[p];
+                mass[u] = sum[p];
             }
 #pragma unroll
             for (int u = 0; u < DEEP; ++u) {
                 const float w = p0 + stride * u < parts
-                                    ? __builtin_amdgcn_exp2f((part[u] - base) * kLog2e)
+                                    ? mass[u] * __builtin_amdgcn_exp2f((part[u] - base) * c2)
                                     : 0.f;
                 total += w;
 #pragma unroll
@@ -313,7 +318,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
         for (int q4 = 0; q4 < 4; ++q4) x[q4] = any ? x[q4] / total : 0.f;
         if (ch < c.d)
             store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch, a.out_bf16, x);
-        if (ch == 0 && a.lse) a.lse[at] = any ? top + __logf(total) : -INFINITY;
+        if (ch == 0 && a.lse)
+            a.lse[at] = any ? fmaf(top, a.scale, __logf(total)) : -INFINITY;
     }
 }
 
@@ -382,7 +388,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
         if (tall && (live > 2 * kCus || parts < 2 * fill)) parts = fill;
         parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
     }
-    const int64_t part_bytes = int64_t(a.q_heads) * a.tokens * (c.d + 1) * 4;
+    const int64_t all_rows = int64_t(a.q_heads) * a.tokens, part_bytes = all_rows * (c.d + 2) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
     // Each workgroup finds its tile among those that have work, where they are few of pairs *
     // tiles: one long sequence among many, whose empty workgroups would cost more (32 heads of
@@ -398,7 +404,9 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     r.plan.step = int((rounds + parts - 1) / parts) * round;
     r.plan.tiles = int(tiles);
     r.plan.parts = int(parts);
-    r.bytes = parts > 1 ? parts * part_bytes : 0;
+    // (in whole units of d + 1 numbers for every row)
+    const int64_t unit = all_rows * (c.d + 1) * 4;
+    r.bytes = parts > 1 ? (parts * part_bytes + unit - 1) / unit * unit : 0;
     return r;
 }
 
@@ -430,7 +438,9 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
     Shape r = shape(a, a.ws ? a.ws_bytes : 0);
     if (r.plan.parts > 1) {
         r.plan.part_o = static_cast<float*>(a.ws);
-        r.plan.part_lse = r.plan.part_o + int64_t(a.q_heads) * a.tokens * r.plan.parts * a.cache.d;
+        const int64_t rows = int64_t(a.q_heads) * a.tokens * r.plan.parts;
+        r.plan.part_sum = r.plan.part_o + rows * a.cache.d;
+        r.plan.part_ref = r.plan.part_sum + rows;
     }
     const hipError_t e = r.rows == 128 ? launch_paged_tiles(a, r.plan, s) : launch_few(a, r, s);
     if (e != hipSuccess || r.plan.parts == 1) return e;

@@ -400,9 +400,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
             const int i = r / G, h = hk * G + r % G;
             const bool any = total > 0.f;
             const float inv = any ? 1.f / total : 0.f;
-            const float lse = !any ? -INFINITY
-                              : lim[n] == kFar ? fmaf(base[n], a.scale, __logf(total))
-                                               : (__log2f(total) - base[n]) * kLn2;
+            const bool far = lim[n] == kFar;
             const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
             const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
                                      : (at * plan.parts + part) * c.d;
@@ -419,10 +417,17 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                     store4(plan.part_o, to + ch, false, x);
             }
             if (g == 0) {
-                if (!whole)
-                    plan.part_lse[at * plan.parts + part] = lse;
-                else if (a.lse)
-                    a.lse[at] = lse;
+                if (!whole) {
+                    // The reference as a score, rounded, and the sum relative to that.
+                    const float ref = far ? base[n] : -base[n] / c2;
+                    const float f = far ? 1.f : __builtin_amdgcn_exp2f(fmaf(-ref, c2, -base[n]));
+                    plan.part_sum[at * plan.parts + part] = any ? total * f : 0.f;
+                    plan.part_ref[at * plan.parts + part] = any ? ref : -INFINITY;
+                } else if (a.lse) {
+                    a.lse[at] = !any  ? -INFINITY
+                                : far ? fmaf(base[n], a.scale, __logf(total))
+                                      : (__log2f(total) - base[n]) * kLn2;
+                }
             }
         }
     }

@@ -10,8 +10,12 @@ namespace sparsp {
 // tiles of all sequences at most, a workgroup finds its own among them instead.
 struct PagedPlan {
     int tiles, parts, step, flat;
-    float* part_o;    // [q_heads, tokens, parts, d]
-    float* part_lse;  // [q_heads, tokens, parts]
+    float* part_o;  // [q_heads, tokens, parts, d], normalised
+    // A part's sum of exponentials [q_heads, tokens, parts], and behind all of them the score, not
+    // yet scaled, that they are relative to (-inf: the part has nothing). Not the log of one times
+    // the other, which a float32 holds to 2^-24 of a row's largest score only: parts of one and of
+    // three equal scores of 2^24 weighed the same.
+    float *part_sum, *part_ref;
 };
 
 // Row tiles of 128 on LDS tiles, bf16 (paged_attn_tiles.hip).

@@ -5,8 +5,6 @@ Q and K are chosen so that every score, and every partial sum of its products, i
 error is what the softmax adds, and the tolerance is that of _cache_ref with e = 0.
 """
 
-import math
-
 import pytest
 import torch
 
@@ -40,7 +38,7 @@ def fill(bt, q_of, k_of):
         bt.K[p, :, r] = k_of(b, t)
 
 
-# dtype, Hq, H, d, page, new, kv: few rows and many, whole and in parts, with an odd end
+# dtype, Hq, H, d, page, new, kv: few rows and many, whole and in parts, an odd last part
 SHAPES = [
     (BF, 4, 1, 128, 64, (1, 2), (77, 2900)),
     (BF, 2, 2, 64, 16, (9, 1), (4100, 20)),
@@ -128,3 +126,22 @@ SCALES = [2.0 ** 60, 2.0 ** 99, 2.0 ** -60]
 @pytest.mark.parametrize("scale", SCALES)
 def test_large_and_small_scales(gpu, dtype, scale):
     scaled_scores(dtype, scale, workspace=False)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("power", POWERS)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_equal_scores_in_parts(gpu, shape, power, sign):
+    equal_scores(*shape, power, sign, workspace=True)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("start", STARTS)
+def test_close_scores_in_parts(gpu, shape, start):
+    close_scores(*shape, start, workspace=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("scale", SCALES)
+def test_scales_in_parts(gpu, dtype, scale):
+    scaled_scores(dtype, scale, workspace=True)
