@@ -11,7 +11,8 @@ Token tensors are [heads, tokens, d] with contiguous channels and any other stri
 projection's [tokens, heads, d] is passed as x.transpose(0, 1). The cache is K_cache and
 V_cache [pages, H, page, d]; page_table int32 [B, width], new_off int32 [B + 1] and kv_len
 int32 [B] (with the new tokens) describe its sequences. Everything is on one GPU; the calls
-run on that GPU's current stream, or on the stream given.
+run on that GPU's current stream, or on the stream given. What a call makes itself (outputs, a
+workspace) comes from the memory of that stream: wait for it before the results are used on another.
 """
 
 from __future__ import annotations
@@ -97,6 +98,22 @@ class Rotary:
         a, b, c = pairs + (0,) * (3 - len(pairs))
         return _ROTARY.pack(self.rot_dim, _LAYOUTS[self.layout], len(pairs), a, b, c, self.factor,
                             inverse)
+
+
+def _make(stream, make, *args, **kwargs):
+    """make(*args, **kwargs): a tensor that a call makes for its work on `stream` (None: the current).
+
+    Memory that the current stream has freed may still be in use there, and would be again once
+    the caller drops this tensor while `stream` works on it; so it comes from the memory of
+    `stream`. The caller goes on with it on the current stream, which the allocator is told.
+    """
+    if stream is None:
+        return make(*args, **kwargs)
+    cuda = _torch().cuda
+    with cuda.stream(stream):
+        t = make(*args, **kwargs)
+    t.record_stream(cuda.current_stream(t.device))
+    return t
 
 
 def _dtype_code(t, name):
@@ -217,13 +234,13 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     if X.dim() != 3 or not X.is_cuda:
         raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
     dev, (_, n, d) = X.get_device(), X.shape
-    y = Y if Y is not None else torch.empty_like(X)
+    y = Y if Y is not None else _make(stream, torch.empty_like, X)
     x, count = _rows(X, "X", dev, X.dtype, n, d), 1
     o = _rows(y, "Y", dev, X.dtype, n, d, X.shape[0])
     y2 = None
     if X2 is not None:
         x += _rows(X2, "X2", dev, X.dtype, n, d)
-        y2 = Y2 if Y2 is not None else torch.empty_like(X2)
+        y2 = Y2 if Y2 is not None else _make(stream, torch.empty_like, X2)
         o += _rows(y2, "Y2", dev, X.dtype, n, d, X2.shape[0])
         count = 2
     elif Y2 is not None:
@@ -275,7 +292,7 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
     if Q is not None:
         q = _rows(Q, "Q", dev, dt, n, d)
         if Q_out is None:
-            Q_out = _torch().empty_like(Q)
+            Q_out = _make(stream, _torch().empty_like, Q)
         qo = _rows(Q_out, "Q_out", dev, dt, n, d, Q.shape[0])
     elif Q_out is not None:
         raise ValueError("Q_out needs Q")
@@ -320,10 +337,10 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     if out_dtype is None:
         out_dtype = _dtype_code(K_cache, "K_cache")
     odt = torch.bfloat16 if out_dtype == BF16 else torch.float32
-    o = O if O is not None else Q.new_empty((heads, n, d), dtype=odt)
+    o = O if O is not None else _make(stream, Q.new_empty, (heads, n, d), dtype=odt)
     ls = lse
     if ls is None and want_lse:
-        ls = Q.new_empty((heads, n), dtype=torch.float32)
+        ls = _make(stream, Q.new_empty, (heads, n), dtype=torch.float32)
     ws, nbytes = None, 0
     if workspace is not None:
         ws = _on(workspace, "workspace", dev)
@@ -374,8 +391,8 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
     B, H, keep = page_table.shape[0], K_cache.shape[1], int(keep)
-    out = kv_len_out if kv_len_out is not None else torch.empty_like(kv_len)
-    lst = kept if kept is not None else kv_len.new_empty((B, H, max(keep, 0)))
+    out = kv_len_out if kv_len_out is not None else _make(stream, torch.empty_like, kv_len)
+    lst = kept if kept is not None else _make(stream, kv_len.new_empty, (B, H, max(keep, 0)))
     dst, dst_width = None, 0
     if dst_table is not None:
         if dst_table.dim() != 2 or dst_table.shape[0] != B:
@@ -385,9 +402,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     if workspace is None:
         nbytes = lib.sparsp_cache_evict_workspace_bytes(c)
         if nbytes > 0:
-            workspace = K_cache.new_empty((nbytes,), dtype=torch.uint8)
-            if stream is not None:
-                workspace.record_stream(stream)
+            workspace = _make(stream, K_cache.new_empty, (nbytes,), dtype=torch.uint8)
     ws = None if workspace is None else _on(workspace, "workspace", dev)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _call(lib.sparsp_cache_evict, dev, stream, c, keep, int(first), int(recent), dst, dst_width,
