@@ -40,6 +40,9 @@ A growing sequence and its paged cache (paged.py, include/sparsp_cache.h):
     sparsp_paged_weights           attention weight per cached token
     sparsp_cache_evict             the cache cut to the tokens of most weight
 
+Calls run on the current stream, or on `stream` where one is given. Outputs that a call makes itself
+come from the memory of that stream: wait for it before they are used on another.
+
 Short aliases without the prefix are provided as well.
 """
 
@@ -289,17 +292,37 @@ def _stream(stream, device):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
-def _outputs(out, like, **specs):
+def _outputs(out, like, stream=None, **specs):
     """A copy of ``out`` (or {}) with a new tensor under every key of specs it lacks."""
     o = dict(out or {})
+    on = () if stream is None else (stream,)
     for key, (shape, dtype) in specs.items():
         if key not in o:
-            o[key] = _empty(shape, dtype, like)
+            o[key] = _empty(shape, dtype, like, *on)
     return o
 
 
-def _empty(shape, dtype, like):
-    return _torch().empty(shape, dtype=dtype, device=like.device)
+def _empty(shape, dtype, like, stream=None):
+    if stream is None:
+        return _torch().empty(shape, dtype=dtype, device=like.device)
+    return _make(stream, _torch().empty, shape, dtype=dtype, device=like.device)
+
+
+def _make(stream, make, *args, **kwargs):
+    """make(*args, **kwargs): a tensor that a call makes for its work on `stream` (None: the current).
+
+    Memory that the current stream has freed may still be in use there, and would be again once
+    the caller drops this tensor while `stream` works on it; so it comes from the memory of
+    `stream`. The caller goes on with it on the current stream, which the allocator is told.
+    """
+    if stream is None:
+        return make(*args, **kwargs)
+    cuda = _torch().cuda
+    with cuda.stream(stream):
+        t = make(*args, **kwargs)
+    if t.is_cuda:  # (what is not is refused later)
+        t.record_stream(cuda.current_stream(t.device))
+    return t
 
 
 # ---------------------------------------------------------------------------
@@ -312,9 +335,9 @@ def sparsp_block_scores(geom: Geometry, Q, K, pooled_q=None, pooled_k=None, scor
     torch = _torch()
     g = geom
     et = _elem_dtype(g)
-    pq = pooled_q if pooled_q is not None else _empty((g.H, g.nq, g.d), torch.float32, Q)
-    pk = pooled_k if pooled_k is not None else _empty((g.H, g.n, g.d), torch.float32, Q)
-    sc = scores if scores is not None else _empty((g.H, g.nq, g.n), torch.float32, Q)
+    pq = pooled_q if pooled_q is not None else _empty((g.H, g.nq, g.d), torch.float32, Q, stream)
+    pk = pooled_k if pooled_k is not None else _empty((g.H, g.n, g.d), torch.float32, Q, stream)
+    sc = scores if scores is not None else _empty((g.H, g.nq, g.n), torch.float32, Q, stream)
     args = (
         _dev(Q, "Q", et, (g.H, g.L, g.d)), _dev(K, "K", et, (g.H, g.L, g.d)),
         _dev(pq, "pooled_q", torch.float32, (g.H, g.nq, g.d)),
@@ -331,8 +354,9 @@ def sparsp_topk_mask(geom: Geometry, scores, keep: int, global_blocks: Sequence[
     """Top-k block mask. Returns (mask uint64-as-int64 [H,nq,W], sel int32 [H,nq,keep])."""
     torch = _torch()
     g = geom
-    m = mask if mask is not None else _empty((g.H, g.nq, g.W), torch.int64, scores)
-    s = sel if sel is not None else _empty((g.H, g.nq, max(int(keep), 0)), torch.int32, scores)
+    m = mask if mask is not None else _empty((g.H, g.nq, g.W), torch.int64, scores, stream)
+    s = sel if sel is not None else _empty((g.H, g.nq, max(int(keep), 0)), torch.int32, scores,
+                                                stream)
     gb = list(int(x) for x in global_blocks)
     arr = (ctypes.c_int32 * max(1, len(gb)))(*gb)
     args = (
@@ -352,9 +376,9 @@ def sparsp_cdf_mask(geom: Geometry, scores, tau: float, global_blocks: Sequence[
     counts int32 [H,nq]); pass sel (its width n is the `keep`) to attention as usual."""
     torch = _torch()
     g = geom
-    m = mask if mask is not None else _empty((g.H, g.nq, g.W), torch.int64, scores)
-    s = sel if sel is not None else _empty((g.H, g.nq, g.n), torch.int32, scores)
-    c = counts if counts is not None else _empty((g.H, g.nq), torch.int32, scores)
+    m = mask if mask is not None else _empty((g.H, g.nq, g.W), torch.int64, scores, stream)
+    s = sel if sel is not None else _empty((g.H, g.nq, g.n), torch.int32, scores, stream)
+    c = counts if counts is not None else _empty((g.H, g.nq), torch.int32, scores, stream)
     gb = list(int(x) for x in global_blocks)
     arr = (ctypes.c_int32 * max(1, len(gb)))(*gb)
     args = (
@@ -382,7 +406,7 @@ def sparsp_demand_union_gather(geom: Geometry, mask, K, V, capacity_blocks: Opti
     g = geom
     et = _elem_dtype(g)
     cap = int(capacity_blocks if capacity_blocks is not None else g.H * g.n)
-    o = _outputs(out, K, demand=((g.H, g.W), torch.int64), head_off=((g.H + 1,), torch.int32),
+    o = _outputs(out, K, stream, demand=((g.H, g.W), torch.int64), head_off=((g.H + 1,), torch.int32),
                  slot_of=((g.H, g.n), torch.int32), gather_blk=((cap,), torch.int32),
                  K_packed=((cap, g.block, g.d), et), V_packed=((cap, g.d, g.block), et))
     args = (
@@ -427,9 +451,9 @@ def sparsp_block_sparse_attn(geom: Geometry, Q, sel, slot_of, K_packed, V_packed
     odt = torch.bfloat16 if out_dtype == BF16 else torch.float32
     if softmax_scale is None:
         softmax_scale = ctypes.c_float(1.0 / math.sqrt(g.d)).value
-    o = O if O is not None else _empty((g.H, g.nq * g.block, g.d), odt, Q)
+    o = O if O is not None else _empty((g.H, g.nq * g.block, g.d), odt, Q, stream)
     ls = lse if lse is not None else (
-        _empty((g.H, g.nq * g.block), torch.float32, Q) if want_lse else None)
+        _empty((g.H, g.nq * g.block), torch.float32, Q, stream) if want_lse else None)
     if K_packed.dim() != 3 or V_packed.dim() != 3:
         raise ValueError("K_packed and V_packed must be 3-D")
     cap = int(K_packed.shape[0])
@@ -478,7 +502,7 @@ def sparsp_row_order(geom: Geometry, counts, order=None, stream=None):
     """Rows h*nq + r sorted by counts (int32 [H, nq]) descending, as int32 [H*nq]."""
     torch = _torch()
     g = geom
-    o = order if order is not None else _empty((g.H * g.nq,), torch.int32, counts)
+    o = order if order is not None else _empty((g.H * g.nq,), torch.int32, counts, stream)
     gs = g.c_struct()
     _check(load_library().sparsp_row_order(ctypes.byref(gs),
                                            _dev(counts, "counts", torch.int32, (g.H, g.nq)),
@@ -542,8 +566,8 @@ def sparsp_block_sparse_attn_part(geom: Geometry, Q, sel, slot_of, K_packed, V_p
     g = geom
     et = _elem_dtype(g)
     keep = int(sel.shape[-1])
-    o = O if O is not None else _empty((g.H, g.nq * g.block, g.d), torch.float32, Q)
-    ls = lse if lse is not None else _empty((g.H, g.nq * g.block), torch.float32, Q)
+    o = O if O is not None else _empty((g.H, g.nq * g.block, g.d), torch.float32, Q, stream)
+    ls = lse if lse is not None else _empty((g.H, g.nq * g.block), torch.float32, Q, stream)
     kp, vp, cap = _packed_args(g, K_packed, V_packed, et)
     args = (
         _dev(Q, "Q", et, (g.H, g.L, g.d)), _dev(sel, "sel", torch.int32, (g.H, g.nq, keep)),
@@ -581,8 +605,8 @@ def sparsp_chunked_attn(geom: Geometry, Q, sel, slot_of, K_packed, V_packed, pla
     et = _elem_dtype(g)
     keep = int(sel.shape[-1])
     so, sl = (g.H, g.nq * g.block, g.d), (g.H, g.nq * g.block)
-    o = O if O is not None else _empty(so, torch.float32, Q)
-    ls = lse if lse is not None else _empty(sl, torch.float32, Q)
+    o = O if O is not None else _empty(so, torch.float32, Q, stream)
+    ls = lse if lse is not None else _empty(sl, torch.float32, Q, stream)
     chunks = [c if isinstance(c, Chunk) else Chunk(*[int(x) for x in c]) for c in plan]
     arr = (Chunk * max(1, len(chunks)))(*chunks)
     kp, vp, cap = _packed_args(g, K_packed, V_packed, et)
@@ -618,7 +642,7 @@ def sparsp_permute_blocks(geom: Geometry, perm, X, Y=None, inverse: bool = False
     torch = _torch()
     g = geom
     et = _elem_dtype(g)
-    y = Y if Y is not None else torch.empty_like(X)
+    y = Y if Y is not None else _make(stream, torch.empty_like, X)
     args = (_dev(perm, "perm", torch.int32, (g.n,)), _dev(X, "X", et, (g.H, g.L, g.d)),
             _dev(y, "Y", et, (g.H, g.L, g.d)), int(bool(inverse)))
     gs = g.c_struct()
@@ -659,7 +683,7 @@ def sparsp_pack_for_consumers(geom: Geometry, demands, ranks: int, producer: int
     nv = (R - 1) * g.H
     lo, hi = (int(producer) * g.n) // R, ((int(producer) + 1) * g.n) // R
     cap = max(1, nv * (hi - lo))
-    o = _outputs(out, K, provide=((nv, g.W), torch.int64), head_off=((nv + 1,), torch.int32),
+    o = _outputs(out, K, stream, provide=((nv, g.W), torch.int64), head_off=((nv + 1,), torch.int32),
                  slot_of=((nv, g.n), torch.int32), gather_blk=((cap,), torch.int32),
                  K_packed=((cap, g.block, g.d), et), V_packed=((cap, g.d, g.block), et))
     args = (

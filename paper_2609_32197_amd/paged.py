@@ -23,7 +23,7 @@ import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
-from . import _SIGNATURES, _RESTYPES, _check, _torch, BF16, F32, load_library
+from . import _SIGNATURES, _RESTYPES, _check, _make, _torch, BF16, F32, load_library
 
 __all__ = [
     "Rotary",
@@ -98,22 +98,6 @@ class Rotary:
         a, b, c = pairs + (0,) * (3 - len(pairs))
         return _ROTARY.pack(self.rot_dim, _LAYOUTS[self.layout], len(pairs), a, b, c, self.factor,
                             inverse)
-
-
-def _make(stream, make, *args, **kwargs):
-    """make(*args, **kwargs): a tensor that a call makes for its work on `stream` (None: the current).
-
-    Memory that the current stream has freed may still be in use there, and would be again once
-    the caller drops this tensor while `stream` works on it; so it comes from the memory of
-    `stream`. The caller goes on with it on the current stream, which the allocator is told.
-    """
-    if stream is None:
-        return make(*args, **kwargs)
-    cuda = _torch().cuda
-    with cuda.stream(stream):
-        t = make(*args, **kwargs)
-    t.record_stream(cuda.current_stream(t.device))
-    return t
 
 
 def _dtype_code(t, name):

@@ -103,3 +103,35 @@ def test_paged_cache(monkeypatch, name, stream):
     made = Made(monkeypatch)
     call(stream)
     check(made.take(), count, stream)
+
+
+def block_calls():
+    g = sp.Geometry(2, 128, 64, 64, 0, 2, sp.BF16)
+    f32, i32, i64 = (dict(dtype=t) for t in (torch.float32, torch.int32, torch.int64))
+    q, sc, mask = gpu(2, 128, 64), gpu(2, 2, 2, **f32), gpu(2, 2, 1, **i64)
+    sel, slot, kp, vp = gpu(2, 2, 2, **i32), gpu(2, 2, **i32), gpu(4, 64, 64), gpu(4, 64, 64)
+    kept = (g, q, sel, slot, kp, vp)
+    return {
+        "scores": (lambda s: sp.sparsp_block_scores(g, q, q, stream=s), 3),
+        "topk": (lambda s: sp.sparsp_topk_mask(g, sc, 1, stream=s), 2),
+        "cdf": (lambda s: sp.sparsp_cdf_mask(g, sc, 0.9, stream=s), 3),
+        "gather": (lambda s: sp.sparsp_demand_union_gather(g, mask, q, q, stream=s), 6),
+        "attention": (lambda s: sp.sparsp_block_sparse_attn(*kept, stream=s), 2),
+        "part": (lambda s: sp.sparsp_block_sparse_attn_part(*kept, (0, 2), (0, 2), stream=s), 2),
+        "chunked": (lambda s: sp.sparsp_chunked_attn(*kept, [], stream=s), 2),
+        "order": (lambda s: sp.sparsp_row_order(g, gpu(2, 2, **i32), stream=s), 1),
+        "permute": (lambda s: sp.sparsp_permute_blocks(g, gpu(2, **i32), q, stream=s), 1),
+        "pack": (lambda s: sp.sparsp_pack_for_consumers(g, gpu(2, 2, 1, **i64), 2, 0, q, q,
+                                                        stream=s), 6),
+    }
+
+
+@pytest.mark.parametrize("name", list(block_calls()))
+@pytest.mark.parametrize("stream", [None, "side"])
+def test_block_calls(monkeypatch, name, stream):
+    call, count = block_calls()[name]
+    monkeypatch.setattr(sp, "_stream", lambda stream, device: None)
+    monkeypatch.setattr(sp, "load_library", Library)
+    made = Made(monkeypatch)
+    call(stream)
+    check(made.take(), count, stream)

@@ -98,3 +98,29 @@ def test_a_step_on_a_side_stream(gpu):
         results.append([x.clone() for x in (r, q, O, lse, w, out, kept, c["K_cache"], c["V_cache"])])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_the_four_calls_on_a_side_stream(gpu):
+    """Scores, mask, gather and attention on a side stream, nothing passed for outputs and all but the
+    last dropped: the same bits as on the current stream."""
+    geom = sp.Geometry(2, 1000, 64, 64, 0, 16, sp.BF16)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn((2, 1000, 64), generator=g, device="cuda").to(BF) for _ in range(3))
+
+    def run(s):
+        sc = sp.sparsp_block_scores(geom, q, k, stream=s)[2]
+        mask, sel = sp.sparsp_topk_mask(geom, sc, 5, stream=s)
+        o = sp.sparsp_demand_union_gather(geom, mask, k, v, stream=s)
+        return sp.sparsp_block_sparse_attn(geom, q, sel, o["slot_of"], o["K_packed"], o["V_packed"],
+                                           stream=s)
+
+    want = run(None)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = run(s)
+        torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.current_stream().wait_stream(s)
+    # (rows behind the sequence's end are no one's)
+    assert torch.equal(got[0][:, :1000], want[0][:, :1000])
+    assert torch.equal(got[1][:, :1000], want[1][:, :1000])
