@@ -33,9 +33,10 @@
  * with the new ones: new token i of n is the cached token kv_len[b] - n + i. Offsets
  * are clamped to [0, tokens], an end below its start to the start, kv_len to
  * [0, width * page]. A page number outside [0, pages) holds no tokens: nothing is read from it
- * or written to it. (new_off ascends; where it does not, columns that two sequences claim hold
- * either one's outputs or none.) Columns before new_off[0] and behind new_off[B] belong to no
- * sequence: their outputs are left as they were.
+ * or written to it. new_off ascends: launches are sized for that, and where it does not, the outputs
+ * in the columns of all sequences, and what is cached and weighed for them, hold any values. Columns
+ * that no sequence claims, among them those before new_off[0] and behind new_off[B], keep their
+ * outputs as they were whatever new_off holds.
  *
  * Limits: d <= 128 (rope alone: 256) and a multiple of 8 (bf16) or 4 (f32); H and
  * query heads <= 1024, query heads a multiple of H; B <= 65536, B * heads <= 2^20; width * page
