@@ -23,7 +23,7 @@
  * Token tensors (sparsp_rows) are [heads, tokens, d] with d contiguous and any
  * strides between heads and tokens: both [H, L, d] and a projection's
  * [tokens, H, d] are read in place. Addresses and strides are multiples of 16
- * bytes.
+ * bytes, strides at least d; rows that a call writes must not overlap.
  *
  * The cache (sparsp_cache) holds K and V as [pages, H, page, d], contiguous:
  * `page` tokens of one head are one contiguous tile, page a power of two in

@@ -40,8 +40,24 @@ int check_type(int d, int dtype, int most) {
     return SPARSP_OK;
 }
 
+// Whether two of a tensor's rows share a channel; both strides are d at least. Heads beside one
+// another behind all tokens, or tokens behind all heads, are seen at once; else the token that begins
+// next to each head's first decides.
+bool rows_overlap(const sparsp_rows* r, int tokens, int d) {
+    const int64_t hs = r->head_stride, ts = r->token_stride;
+    if (r->heads < 2 || tokens < 2) return false;
+    if ((hs - d) / ts >= tokens - 1 || (ts - d) / hs >= r->heads - 1) return false;
+    for (int64_t at = hs; at < r->heads * hs; at += hs) {
+        const int64_t t = at / ts;
+        if (t < tokens && at - t * ts < d) return true;
+        if (t + 1 < tokens && (t + 1) * ts - at < d) return true;
+    }
+    return false;
+}
+
 // A [heads, tokens, d] tensor of elements of `size` bytes.
-int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int size) {
+int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int size,
+               bool written = false) {
     if (!r || !r->data) return fail(SPARSP_E_INVALID, "%s is NULL", name);
     if (r->heads < 1 || r->heads > 1024)
         return fail(SPARSP_E_UNSUPPORTED, "%s has %d heads, 1 to 1024 are supported", name, r->heads);
@@ -51,7 +67,9 @@ int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int si
     if (r->head_stride < 0 || r->token_stride < 0 || r->head_stride > most || r->token_stride > most)
         return fail(SPARSP_E_INVALID, "%s: stride out of range", name);
     if ((tokens > 1 && r->token_stride < d) || (r->heads > 1 && r->head_stride < d))
-        return fail(SPARSP_E_INVALID, "%s: rows must not overlap (strides below d = %d)", name, d);
+        return fail(SPARSP_E_INVALID, "%s: strides below d = %d", name, d);
+    if (written && rows_overlap(r, tokens, d))
+        return fail(SPARSP_E_INVALID, "%s: its rows overlap", name);
     return SPARSP_OK;
 }
 
@@ -232,7 +250,7 @@ int sparsp_rope(const sparsp_rotary* r, int32_t tokens, int32_t d, int32_t dtype
     const int size = dtype == SPARSP_BF16 ? 2 : 4;
     for (int k = 0; k < count; ++k) {
         if (int rc = check_rows(x + k, "X", tokens, d, size)) return rc;
-        if (int rc = check_rows(y + k, "Y", tokens, d, size)) return rc;
+        if (int rc = check_rows(y + k, "Y", tokens, d, size, true)) return rc;
         if (int rc = check_same_rows(x + k, y + k, "X")) return rc;
         a.move[k] = row_move(x[k], y[k], true);
     }
@@ -267,7 +285,7 @@ int sparsp_paged_append(const sparsp_cache* cache, int32_t tokens, const sparsp_
     a.moves = 2;
     if (Q) {
         if (int rc = check_rows(Q, "Q", tokens, cache->d, size)) return rc;
-        if (int rc = check_rows(Q_out, "Q_out", tokens, cache->d, size)) return rc;
+        if (int rc = check_rows(Q_out, "Q_out", tokens, cache->d, size, true)) return rc;
         if (int rc = check_same_rows(Q, Q_out, "Q")) return rc;
         a.move[a.moves++] = row_move(*Q, *Q_out, true);
     }
@@ -302,7 +320,7 @@ int sparsp_paged_attn(const sparsp_cache* cache, int32_t tokens, const sparsp_ro
         return fail(SPARSP_E_DTYPE, "unknown out_dtype %d", out_dtype);
     if (cache->dtype == SPARSP_F32 && out_dtype != SPARSP_F32)
         return fail(SPARSP_E_DTYPE, "f32 inputs produce f32 output only");
-    if (int rc = check_rows(O, "O", tokens, cache->d, out_dtype == SPARSP_BF16 ? 2 : 4)) return rc;
+    if (int rc = check_rows(O, "O", tokens, cache->d, out_dtype == SPARSP_BF16 ? 2 : 4, true)) return rc;
     if (O->heads != Q->heads)
         return fail(SPARSP_E_INVALID, "O has %d heads, Q has %d", O->heads, Q->heads);
     if (O->data == Q->data) return fail(SPARSP_E_INVALID, "O may not be Q");
