@@ -132,7 +132,8 @@ typedef struct {
  * Writes the new tokens' K and V [H, tokens, d] into the cache, and 0 into their
  * weights where cache.weights is given. With a rotation r, K is rotated on the way
  * (as by sparsp_rope), and so is Q into Q_out where Q is given (Q_out may be Q).
- * Without r, Q must be NULL. A token whose place has no page, or lies before the first
+ * Without r, Q must be NULL. Q_out and Q apart, nothing that is written may overlap another
+ * tensor, nor K of the cache its V. A token whose place has no page, or lies before the first
  * cached token (kv_len < n), is not written; its Q is rotated all the same. Places
  * that two tokens share (a page in two tables) hold either one's values.
  */
@@ -204,8 +205,8 @@ int sparsp_paged_weights(const sparsp_cache* cache, int32_t tokens, const sparsp
  * dst_table NULL: within the sequence's own pages. Otherwise int32 [B, dst_width] with
  * dst_width * page >= keep: the kept tokens go to those pages of the same cache, none of
  * which may be a page of `table`, and the old pages stay as they were. Pages must not be
- * shared between sequences (or heads would move twice). A token on a bad page weighs as NaN and
- * moves nothing. first + recent <= keep; keep >= 1.
+ * shared between sequences, nor K with V (or rows would move twice). A token on a bad page weighs
+ * as NaN and moves nothing. first + recent <= keep; keep >= 1.
  *
  * workspace: 16-byte aligned device memory or NULL, contents irrelevant, not shared by calls that
  * overlap. With sparsp_cache_evict_workspace_bytes bytes the choice in few long sequences is

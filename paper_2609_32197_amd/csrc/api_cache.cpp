@@ -102,6 +102,12 @@ int check_pointers(const sparsp_cache* c, bool values, bool weights, bool batch)
     return SPARSP_OK;
 }
 
+// For calls that write both.
+int check_apart(const sparsp_cache* c) {
+    if (c->K == c->V) return fail(SPARSP_E_INVALID, "K and V of the cache are the same memory");
+    return SPARSP_OK;
+}
+
 int check_tokens(int tokens) {
     if (tokens < 0 || tokens > (1 << 26))
         return fail(SPARSP_E_INVALID, "tokens = %d outside [0, 2^26]", tokens);
@@ -254,6 +260,10 @@ int sparsp_rope(const sparsp_rotary* r, int32_t tokens, int32_t d, int32_t dtype
         if (int rc = check_same_rows(x + k, y + k, "X")) return rc;
         a.move[k] = row_move(x[k], y[k], true);
     }
+    // (empty tensors have no address of their own)
+    if (tokens > 0 && count == 2 &&
+        (y[0].data == y[1].data || y[0].data == x[1].data || y[1].data == x[0].data))
+        return fail(SPARSP_E_INVALID, "an output is the other output or the other's input");
     if (tokens == 0) return ok();
     a.moves = count;
     a.tokens = tokens;
@@ -270,6 +280,7 @@ int sparsp_paged_append(const sparsp_cache* cache, int32_t tokens, const sparsp_
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_tokens(tokens)) return rc;
     if (int rc = check_pointers(cache, true, false, true)) return rc;
+    if (int rc = check_apart(cache)) return rc;
     const int size = cache->dtype == SPARSP_BF16 ? 2 : 4;
     if (int rc = check_rows(K, "K", tokens, cache->d, size)) return rc;
     if (int rc = check_rows(V, "V", tokens, cache->d, size)) return rc;
@@ -363,9 +374,12 @@ int sparsp_cache_evict(const sparsp_cache* cache, int32_t keep, int32_t first, i
                        int32_t* kept, void* workspace, int64_t workspace_bytes, void* stream) {
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_pointers(cache, true, true, false)) return rc;
+    if (int rc = check_apart(cache)) return rc;
     if (!kv_len_out || !kept) return fail(SPARSP_E_INVALID, "kv_len_out or kept is NULL");
     if (kv_len_out == cache->kv_len)
         return fail(SPARSP_E_INVALID, "kv_len_out may not be the cache's kv_len");
+    if (kept == cache->kv_len || kept == kv_len_out)
+        return fail(SPARSP_E_INVALID, "kept may not be a list of lengths");
     if (keep < 1 || keep > (1 << 30)) return fail(SPARSP_E_INVALID, "keep = %d must be positive", keep);
     if (first < 0 || recent < 0 || int64_t(first) + recent > keep)
         return fail(SPARSP_E_INVALID, "first = %d and recent = %d must fit into keep = %d", first,

@@ -32,3 +32,7 @@ def run_check(tmp_path, name):
 
 def test_rows_that_overlap(tmp_path):
     run_check(tmp_path, "cache_rows_check")
+
+
+def test_tensors_given_twice(tmp_path):
+    run_check(tmp_path, "cache_alias_check")
