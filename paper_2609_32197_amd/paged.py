@@ -100,6 +100,18 @@ class Rotary:
                             inverse)
 
 
+def _int(x, name):
+    """x as an int of 32 bits; ctypes would cut a larger one to its low bits."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} = {x} does not fit into 32 bits")
+    return x
+
+
+def _hints(max_new, max_kv):
+    return _int(max_new or 0, "max_new"), _int(max_kv or 0, "max_kv")
+
+
 def _dtype_code(t, name):
     torch = _torch()
     if t.dtype == torch.bfloat16:
@@ -194,9 +206,10 @@ def sparsp_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str =
     import numpy as np
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(_SCALINGS)} (got {scaling!r})")
-    f = np.empty(max(1, int(rot_dim) // 2), dtype=np.float32)
+    rot_dim = _int(rot_dim, "rot_dim")
+    f = np.empty(min(max(1, rot_dim // 2), 128), dtype=np.float32)  # (longer ones are refused)
     factor = ctypes.c_float()
-    _check(load_library().sparsp_rope_frequencies(int(rot_dim), float(theta), _SCALINGS[scaling],
+    _check(load_library().sparsp_rope_frequencies(rot_dim, float(theta), _SCALINGS[scaling],
                                                   float(scale), float(trained), float(low),
                                                   float(high), f.ctypes.data,
                                                   ctypes.addressof(factor)))
@@ -291,8 +304,8 @@ def sparsp_paged_attn_workspace_bytes(K_cache, page_table, tokens: int, q_heads:
     B, width = page_table.shape
     P, H, page, d = K_cache.shape
     c = _CACHE.pack(0, 0, 0, 0, 0, 0, P, H, page, d, _dtype_code(K_cache, "K_cache"), width, B, 0)
-    n = int(load_library().sparsp_paged_attn_workspace_bytes(c, int(tokens), int(q_heads),
-                                                            int(max_new or 0), int(max_kv or 0)))
+    n = int(load_library().sparsp_paged_attn_workspace_bytes(
+        c, _int(tokens, "tokens"), _int(q_heads, "q_heads"), *_hints(max_new, max_kv)))
     _check(n if n < 0 else 0)
     return n
 
@@ -330,9 +343,9 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
         ws = _on(workspace, "workspace", dev)
         nbytes = workspace.numel() * workspace.element_size()
     _call(load_library().sparsp_paged_attn, dev, stream, c, n, _rows(Q, "Q", dev, dt, n, d),
-          _rows(o, "O", dev, odt, n, d, heads), int(out_dtype),
+          _rows(o, "O", dev, odt, n, d, heads), _int(out_dtype, "out_dtype"),
           None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
-          bool(causal), _scale(softmax_scale, d), int(max_new or 0), int(max_kv or 0), ws, nbytes)
+          bool(causal), _scale(softmax_scale, d), *_hints(max_new, max_kv), ws, nbytes)
     return o, ls
 
 
@@ -357,7 +370,7 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
     _call(load_library().sparsp_paged_weights, dev, stream, c, n,
           _rows(Q, "Q", dev, K_cache.dtype, n, d),
           _on(lse, "lse", dev, torch.float32, (heads, n)) or 16, bool(causal),
-          _scale(softmax_scale, d), bool(accumulate), int(max_new or 0), int(max_kv or 0))
+          _scale(softmax_scale, d), bool(accumulate), *_hints(max_new, max_kv))
     return weights
 
 
@@ -374,7 +387,8 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
-    B, H, keep = page_table.shape[0], K_cache.shape[1], int(keep)
+    B, H = page_table.shape[0], K_cache.shape[1]
+    keep, first, recent = _int(keep, "keep"), _int(first, "first"), _int(recent, "recent")
     out = kv_len_out if kv_len_out is not None else _make(stream, torch.empty_like, kv_len)
     lst = kept if kept is not None else _make(stream, kv_len.new_empty, (B, H, max(keep, 0)))
     dst, dst_width = None, 0
@@ -389,7 +403,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
             workspace = _make(stream, K_cache.new_empty, (nbytes,), dtype=torch.uint8)
     ws = None if workspace is None else _on(workspace, "workspace", dev)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call(lib.sparsp_cache_evict, dev, stream, c, keep, int(first), int(recent), dst, dst_width,
+    _call(lib.sparsp_cache_evict, dev, stream, c, keep, first, recent, dst, dst_width,
           _on(out, "kv_len_out", dev, torch.int32, (B,)),
           _on(lst, "kept", dev, torch.int32, (B, H, max(keep, 0))), ws, nbytes)
     return out, lst
