@@ -94,7 +94,8 @@ typedef struct {
  *           g = clamp((r - low) / (high - low), 0, 1):  f_p (g + (1 - g) / scale),
  *           and *factor = 0.1 ln(scale) + 1
  * *factor is 1 otherwise. Computed in 64 bits, rounded to float32 once. scale >= 1;
- * PARTS needs trained > 0 and low < high; BASE needs rot_dim > 2. Pure host code.
+ * PARTS needs trained > 0 and low < high; BASE needs rot_dim > 2. A frequency past float32's range
+ * (theta far below 1) is an error. Pure host code.
  */
 int sparsp_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double scale,
                             double trained, double low, double high, float* inv_freq,

@@ -239,6 +239,8 @@ int sparsp_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, doub
             f *= g + (1.0 - g) / scale;
         }
         inv_freq[p] = float(f);
+        if (!std::isfinite(inv_freq[p]))
+            return fail(SPARSP_E_INVALID, "theta = %g: frequency %d is no float32", theta, p);
     }
     *factor = scaling == SPARSP_ROPE_PARTS ? float(0.1 * std::log(scale) + 1.0) : 1.0f;
     return ok();
