@@ -140,7 +140,6 @@ int check_rotary(const sparsp_rotary* r, int d, const void* positions, int bits,
         return fail(SPARSP_E_DTYPE, "position_bits = %d must be 32 or 64", bits);
     a->rot = r->rot_dim;
     a->layout = r->layout;
-    a->axes = r->axes;
     a->factor = r->factor;
     a->inverse = r->inverse != 0;
     a->positions = positions;

@@ -30,7 +30,7 @@ struct RotateArgs {
     int tokens = 0, d = 0;
     bool bf16 = false;
     // Rotation; rot = 0 moves rows as they are.
-    int rot = 0, layout = 0, axes = 1;
+    int rot = 0, layout = 0;
     int axis_end[3] = {};  // pairs before axis_end[a] turn with axis a or an earlier one
     float factor = 1.f;
     bool inverse = false;

@@ -17,7 +17,6 @@
 #include <algorithm>
 #include <cmath>
 
-#include "paged_plan.h"
 #include "paged_tiles.h"
 
 namespace sparsp {
@@ -394,7 +393,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     // tiles: one long sequence among many, whose empty workgroups would cost more (32 heads of
     // 128, 256 sequences of one new token and one of 1,024 over 2,000 each: 900 us, 386 us; the
     // two kinds by themselves: 356 and 58 us). And where key heads leave XCDs less to do than
-    // others (2 of 128, 2,000 tokens over 6,000: 203 us, 110 us; 5 of 64: 187 and 138 us; 4
+    // others (2 of 128, 2,000 tokens over 6,000: 203 us, 115 us; 5 of 64: 187 and 138 us; 4
     // sequences of 806 to 2,000 tokens, 2 heads: 184 and 115 us), but not like sequences that
     // fill all eight (4 of 2,000 tokens, 2 heads: 53 and 60 us).
     const bool even = a.tokens == int64_t(c.B) * most_new && parts == 1 && pairs % 8 == 0;

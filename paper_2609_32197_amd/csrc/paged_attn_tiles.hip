@@ -28,34 +28,14 @@
 namespace sparsp {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx8 __attribute__((ext_vector_type(8)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
-typedef short short8_t __attribute__((ext_vector_type(8)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t lds_short4;
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 constexpr int kKeys = 64;        // keys of a tile
 constexpr int kRowsTile = 128;   // rows of a workgroup
 constexpr int kSegment = 16384;  // keys whose page numbers are held at once
-
-// Max and sum over the four lanes that hold a row.
-__device__ __forceinline__ float quad_max(float x) {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
 
 // The XOR of a row's 16-byte chunk number, for K and for V.
 template <int D>
@@ -337,7 +317,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                             float mx = -INFINITY;
 #pragma unroll
                             for (int v = 0; v < 8; ++v) mx = fmaxf(mx, sc[n][2 * t + v / 4][v % 4]);
-                            mx = quad_max(mx);
+                            mx = row_max(mx);
                             // A reference of 2^24 and more in log2 units is rounded by a half and
                             // more, one of 2^32 by more than an exponential can make good. Such a
                             // row keeps its reference as a score and subtracts that first, in this
@@ -395,7 +375,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int r = tile * kRowsTile + wave * 32 + n * 16 + col;
-            const float total = quad_sum(l[n]);
+            const float total = row_sum(l[n]);
             if (r >= rows) continue;
             const int i = r / G, h = hk * G + r % G;
             const bool any = total > 0.f;

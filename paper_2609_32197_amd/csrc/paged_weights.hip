@@ -21,7 +21,6 @@
 // 300: 26 us, 76 us; 2,000 over 2,000: 373 and 511 us; 64 over 8,000: 87 and 80 us).
 #include <algorithm>
 
-#include "paged_plan.h"
 #include "paged_tiles.h"
 
 namespace sparsp {

@@ -18,11 +18,6 @@
 namespace sparsp {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRows = 64;   // rows of a tile
 constexpr int kKeys = 256;  // keys of a workgroup
 

@@ -32,7 +32,7 @@ struct Move {
 
 struct Params {
     Move move[3];
-    int moves, tokens, d, P, layout, inverse, wide, stream;
+    int moves, tokens, d, P, inverse, wide, stream;
     Div per;  // tokens of a workgroup
     int axis_end[3];
     float factor;
@@ -229,7 +229,6 @@ hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
     p.tokens = a.tokens;
     p.d = a.d;
     p.P = a.rot / 2;
-    p.layout = a.layout;
     p.inverse = a.inverse;
     p.wide = a.wide;
     for (int x = 0; x < 3; ++x) p.axis_end[x] = a.axis_end[x];
