@@ -154,8 +154,9 @@ int sparsp_paged_append(const sparsp_cache* cache, int32_t tokens, const sparsp_
  * Q, O: [heads, tokens, d]; O in out_dtype (F32 always; BF16, rounded to nearest even,
  * for a bf16 cache). lse: float32 [heads, tokens] or NULL. (O as [heads, tokens, d] and
  * lse are what sparsp_lse_merge takes, so parts over several caches can be joined.)
- * bf16 products run on the matrix cores with float32 sums, probabilities rounded to bf16;
- * softmax statistics are float32. f32 products are float32. The largest score of a row is subtracted
+ * bf16 products run on the matrix cores with float32 sums. Where max_new has at most 16 rows (tokens
+ * times query heads of a key head; 32 for d <= 64) probabilities enter them to 2^-16 of themselves,
+ * otherwise rounded to bf16; softmax statistics are float32. f32 products are float32. The largest score of a row is subtracted
  * from the others before anything is rounded to its size, however large it is, in whole rows and
  * in split ones; lse itself is one float32. Q, and K and V where a
  * row's sequence has tokens, must be finite; what lies in the cache outside a sequence's
