@@ -155,12 +155,12 @@ int sparsp_paged_append(const sparsp_cache* cache, int32_t tokens, const sparsp_
  * for a bf16 cache). lse: float32 [heads, tokens] or NULL. (O as [heads, tokens, d] and
  * lse are what sparsp_lse_merge takes, so parts over several caches can be joined.)
  * bf16 products run on the matrix cores with float32 sums. Where max_new has at most 16 rows (tokens
- * times query heads of a key head; 32 for d <= 64) probabilities enter them to 2^-16 of themselves,
- * otherwise rounded to bf16; softmax statistics are float32. f32 products are float32. The largest score of a row is subtracted
- * from the others before anything is rounded to its size, however large it is, in whole rows and
- * in split ones; lse itself is one float32. Q, and K and V where a
- * row's sequence has tokens, must be finite; what lies in the cache outside a sequence's
- * tokens does not matter.
+ * times query heads of a key head; 32 for d <= 64) probabilities enter them to 2^-16 of
+ * themselves, otherwise rounded to bf16; softmax statistics are float32. f32 products are
+ * float32. The largest score of a row is subtracted from the others before anything is rounded to
+ * its size, however large it is, in whole rows and in split ones; lse itself is one float32. Q,
+ * and K and V where a row's sequence has tokens, must be finite; what lies in the cache outside a
+ * sequence's tokens does not matter.
  *
  * max_new, max_kv: what the caller knows of the largest number of new tokens and of cached
  * tokens of a sequence (0: nothing). They size the launch; results are right for
@@ -186,10 +186,9 @@ int64_t sparsp_paged_attn_workspace_bytes(const sparsp_cache* cache, int32_t tok
  *   exp(scale q.k_t - lse[head, token])
  * added (accumulate != 0) or written: the attention weight it received in this step,
  * with Q, lse, causal and scale as in sparsp_paged_attn. A row of lse = -inf adds
- * nothing. (lse is a float32: a weight is off by up to 2^-24 |lse| of itself, whatever
- * rounds it.) Weights of other places stay. Sums are float32 in an order that depends on the
- * arguments only. A sequence without new tokens gets 0 added. Pages must not be shared
- * between sequences.
+ * nothing. (lse is a float32, and a weight off by up to 2^-22 |lse| of itself.) Weights of
+ * other places stay. Sums are float32 in an order that depends on the arguments only. A
+ * sequence without new tokens gets 0 added. Pages must not be shared between sequences.
  */
 int sparsp_paged_weights(const sparsp_cache* cache, int32_t tokens, const sparsp_rows* Q,
                          const float* lse, int32_t causal, float softmax_scale,
