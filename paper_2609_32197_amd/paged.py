@@ -103,13 +103,25 @@ class Rotary:
 def _int(x, name):
     """x as an int of 32 bits; ctypes would cut a larger one to its low bits."""
     x = int(x)
-    if not -2 ** 31 <= x < 2 ** 31:
+    if not -0x80000000 <= x < 0x80000000:
         raise ValueError(f"{name} = {x} does not fit into 32 bits")
     return x
 
 
 def _hints(max_new, max_kv):
     return _int(max_new or 0, "max_new"), _int(max_kv or 0, "max_kv")
+
+
+def _like(t, stream):
+    if stream is None:
+        return _torch().empty_like(t)
+    return _make(stream, _torch().empty_like, t)
+
+
+def _new(t, shape, dtype, stream):
+    if stream is None:
+        return t.new_empty(shape, dtype=dtype)
+    return _make(stream, t.new_empty, shape, dtype=dtype)
 
 
 def _dtype_code(t, name):
@@ -231,13 +243,13 @@ def sparsp_rope(rotary: Rotary, X, positions, inv_freq, X2=None, Y=None, Y2=None
     if X.dim() != 3 or not X.is_cuda:
         raise ValueError("X must be a [heads, tokens, d] tensor on the GPU")
     dev, (_, n, d) = X.get_device(), X.shape
-    y = Y if Y is not None else _make(stream, torch.empty_like, X)
+    y = Y if Y is not None else _like(X, stream)
     x, count = _rows(X, "X", dev, X.dtype, n, d), 1
     o = _rows(y, "Y", dev, X.dtype, n, d, X.shape[0])
     y2 = None
     if X2 is not None:
         x += _rows(X2, "X2", dev, X.dtype, n, d)
-        y2 = Y2 if Y2 is not None else _make(stream, torch.empty_like, X2)
+        y2 = Y2 if Y2 is not None else _like(X2, stream)
         o += _rows(y2, "Y2", dev, X.dtype, n, d, X2.shape[0])
         count = 2
     elif Y2 is not None:
@@ -289,7 +301,7 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
     if Q is not None:
         q = _rows(Q, "Q", dev, dt, n, d)
         if Q_out is None:
-            Q_out = _make(stream, _torch().empty_like, Q)
+            Q_out = _like(Q, stream)
         qo = _rows(Q_out, "Q_out", dev, dt, n, d, Q.shape[0])
     elif Q_out is not None:
         raise ValueError("Q_out needs Q")
@@ -334,10 +346,10 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     if out_dtype is None:
         out_dtype = _dtype_code(K_cache, "K_cache")
     odt = torch.bfloat16 if out_dtype == BF16 else torch.float32
-    o = O if O is not None else _make(stream, Q.new_empty, (heads, n, d), dtype=odt)
+    o = O if O is not None else _new(Q, (heads, n, d), odt, stream)
     ls = lse
     if ls is None and want_lse:
-        ls = _make(stream, Q.new_empty, (heads, n), dtype=torch.float32)
+        ls = _new(Q, (heads, n), torch.float32, stream)
     ws, nbytes = None, 0
     if workspace is not None:
         ws = _on(workspace, "workspace", dev)
@@ -389,8 +401,8 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
     B, H = page_table.shape[0], K_cache.shape[1]
     keep, first, recent = _int(keep, "keep"), _int(first, "first"), _int(recent, "recent")
-    out = kv_len_out if kv_len_out is not None else _make(stream, torch.empty_like, kv_len)
-    lst = kept if kept is not None else _make(stream, kv_len.new_empty, (B, H, max(keep, 0)))
+    out = kv_len_out if kv_len_out is not None else _like(kv_len, stream)
+    lst = kept if kept is not None else _new(kv_len, (B, H, max(keep, 0)), torch.int32, stream)
     dst, dst_width = None, 0
     if dst_table is not None:
         if dst_table.dim() != 2 or dst_table.shape[0] != B:
@@ -400,7 +412,7 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     if workspace is None:
         nbytes = lib.sparsp_cache_evict_workspace_bytes(c)
         if nbytes > 0:
-            workspace = _make(stream, K_cache.new_empty, (nbytes,), dtype=torch.uint8)
+            workspace = _new(K_cache, (nbytes,), torch.uint8, stream)
     ws = None if workspace is None else _on(workspace, "workspace", dev)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _call(lib.sparsp_cache_evict, dev, stream, c, keep, first, recent, dst, dst_width,
