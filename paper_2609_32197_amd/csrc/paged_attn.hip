@@ -13,7 +13,8 @@
 //
 // Long caches are split: each part (a multiple of `step` keys) writes its normalised
 // output, its sum of exponentials and the score they are relative to, float32, to the workspace,
-// and a merge kernel joins a row's parts in their order. A sequence short enough for one part writes its output directly.
+// and a merge kernel joins a row's parts in their order. A sequence short enough for one part writes
+// its output directly.
 #include <algorithm>
 #include <cmath>
 

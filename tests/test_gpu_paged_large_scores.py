@@ -8,7 +8,6 @@ error is what the softmax adds, and the tolerance is that of _cache_ref with e =
 import pytest
 import torch
 
-import paper_2609_32197_amd as sp
 from tests import _cache_ref as R
 from tests.test_gpu_paged_attn import BF, F, run
 
