@@ -49,6 +49,7 @@ struct PagedArgs {
     bool causal;
     float scale;
     int max_new, max_kv;
+    int window, sinks;  // window 0: none
     // attention
     void* O;
     int64_t o_head, o_token;

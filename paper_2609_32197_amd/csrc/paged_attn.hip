@@ -26,7 +26,7 @@ namespace {
 constexpr int kCus = 256;
 constexpr int kSegment = 16384;  // keys whose page numbers are held at once
 
-template <typename T, int D, int NC>
+template <typename T, int D, int NC, bool WINDOW>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, const PagedPlan plan) {
     using M = TileMath<T, D>;
     constexpr int KEYS = M::KEYS, DV = M::DV, PITCH = D + 4;
@@ -42,16 +42,29 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
-    const int keys = part_keys(plan, s.kv);
-    const bool whole = s.kv <= keys;
-    if (part > 0 && part * int64_t(keys) >= s.kv) return;
-    const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
+    Span span = {0, 0, s.kv, 0};
+    int keys = part_keys(plan, s.kv);
+    bool whole = s.kv <= keys;
+    if (!WINDOW && part > 0 && part * int64_t(keys) >= s.kv) return;
+    int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
     const float c2 = a.scale * kLog2e;
     const int shift = __builtin_ctz(c.page);
+    // Entries of the page list: pages, or with a window 16 keys each (the gap is no multiple of
+    // a page).
+    const int list_shift = WINDOW ? 4 : shift;
 
     for (int tile = work.tile; tile * int64_t(16 * NC) < rows; tile += work.stride) {
+        if constexpr (WINDOW) {
+            span = span_of(a, s, G, tile * 16 * NC, min(rows, (tile + 1) * 16 * NC) - 1, KEYS);
+            keys = part_keys(plan, span.len);
+            whole = span.len <= keys;
+            if (part > 0 && part * int64_t(keys) >= span.len) continue;
+            lo = part * keys;
+            part_end = min(span.len - lo, keys) + lo;
+        }
         typename M::QTile q[NC];
         int limit[NC], lowest = 1 << 30;  // keys before limit are seen
+        int first[NC], latest = 0;        // with a window, those from first on and the sinks
         int end = 0;
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
@@ -59,6 +72,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             const bool live = r < rows;
             const int i = live ? r / G : 0, h = hk * G + (live ? r % G : 0);
             limit[n] = a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+            if constexpr (WINDOW) {
+                limit[n] -= span.skip;
+                first[n] = live ? limit[n] - a.window : 0;
+                latest = max(latest, first[n]);
+            }
             if (!live) limit[n] = 1 << 30;
             lowest = min(lowest, limit[n]);
             M::load_row(q[n], a.Q, int64_t(h) * a.q_head + int64_t(s.q0 + i) * a.q_token, live,
@@ -67,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
         {
             const int last = min(rows, (tile + 1) * 16 * NC) - 1;
             end = a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv;
-            end = min(end, part_end);
+            end = min(end - span.skip, part_end);
         }
 
         floatx4 acc[NC][DV];
@@ -86,17 +104,18 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
             int kp, vp;
         };
         auto load_k = [&](Stage& st, int t0, int p0) {
-            st.kp = page_list[((t0 + M::k_group(lane)) >> shift) - p0];
-            M::load_k(c, st.k, st.kp, hk, t0, lane);
+            st.kp = page_list[((t0 + M::k_group(lane)) >> list_shift) - p0];
+            M::load_k(c, st.k, st.kp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         auto load_v = [&](Stage& st, int t0, int p0) {
-            st.vp = page_list[((t0 + M::v_group(lane)) >> shift) - p0];
-            M::load_v(c, st.v, st.vp, hk, t0, lane);
+            st.vp = page_list[((t0 + M::v_group(lane)) >> list_shift) - p0];
+            M::load_v(c, st.v, st.vp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         // after_scores: what is done once K has been used.
         auto compute = [&](Stage& st, int t0, auto after_scores) {
             const bool masked =
-                __ballot(t0 + KEYS > lowest || t0 + KEYS > end || st.kp < 0 || st.vp < 0) != 0;
+                __ballot(t0 + KEYS > lowest || t0 + KEYS > end || st.kp < 0 || st.vp < 0 ||
+                         (WINDOW && t0 < latest && t0 + KEYS > a.sinks)) != 0;
             if (masked) {
                 // What lies behind the sequence may be anything, NaN included: rows of V there
                 // are zeroed, not multiplied by a probability of zero.
@@ -116,8 +135,12 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
                 if (masked) {
                     const int lim = st.vp < 0 ? 0 : min(limit[n], part_end);
 #pragma unroll
-                    for (int v = 0; v < M::PER; ++v)
-                        p[v] = t0 + M::key_of(g, v) < lim ? p[v] : -INFINITY;
+                    for (int v = 0; v < M::PER; ++v) {
+                        const int key = t0 + M::key_of(g, v);
+                        const bool seen =
+                            key < lim && (!WINDOW || key >= first[n] || key < a.sinks);
+                        p[v] = seen ? p[v] : -INFINITY;
+                    }
                 }
                 float mx = p[0];
 #pragma unroll
@@ -149,11 +172,16 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
         // them would return in order with the rows asked for before.
         constexpr int JUMP = 4 * KEYS;
         for (int seg = lo; seg < end; seg += kSegment) {
-            const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
-            const int entries = ((((seg_end + JUMP - 1) & -JUMP) - 1) >> shift) - p0 + 1;
+            const int seg_end = min(end, seg + kSegment), p0 = seg >> list_shift;
+            const int entries = ((((seg_end + JUMP - 1) & -JUMP) - 1) >> list_shift) - p0 + 1;
             __syncthreads();  // the list before has been read
-            for (int e = threadIdx.x; e < entries; e += 256)
-                page_list[e] = page_of(c.table, c.width, c.pages, b, p0 + e);
+            for (int e = threadIdx.x; e < entries; e += 256) {
+                const int key = (p0 + e) << list_shift;
+                const int j = WINDOW ? span.cached(key) >> shift : p0 + e;
+                page_list[e] = WINDOW && !span.sees(key, a.sinks)
+                                   ? -1
+                                   : page_of(c.table, c.width, c.pages, b, j);
+            }
             __syncthreads();
             int t0 = seg + wave * KEYS;
             if (t0 >= seg_end) continue;
@@ -247,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
 // rows: the eight groups of a workgroup take one row's parts in turn and are added in LDS in
 // their order. Otherwise each group has a row of its own (16,384 rows of two parts: 27 us with
 // the attention, 50 us with a workgroup for each row).
-template <bool SHARED>
+template <bool SHARED, bool WINDOW>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, const PagedPlan plan,
                                                           int per_head) {
     __shared__ float part_x[8][128];
@@ -256,15 +284,23 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     const int bh = blockIdx.x / per_head;
     const int b = bh / a.q_heads, h = bh % a.q_heads;
     const Seq s = sequence(c, a.tokens, b);
-    const int keys = part_keys(plan, s.kv);
-    if (s.kv <= keys) return;
-    const int parts = (s.kv + keys - 1) / keys;
+    int keys = part_keys(plan, s.kv);
+    if (!WINDOW && s.kv <= keys) return;
+    int parts = (s.kv + keys - 1) / keys;
     const float c2 = a.scale * kLog2e;
     const int group = threadIdx.x >> 5, lane = threadIdx.x & 31, ch = lane * 4;
     const int first = SHARED ? group : 0, stride = SHARED ? 8 : 1;  // of a group's parts
     constexpr int ROWS = SHARED ? 1 : 8, DEEP = 4;                  // DEEP parts in flight
     for (int i0 = blockIdx.x % per_head * ROWS; i0 < s.n; i0 += per_head * ROWS) {
         const int i = SHARED ? i0 : min(i0 + group, s.n - 1);
+        if constexpr (WINDOW) {  // what the row's tile has walked
+            const int G = a.q_heads / c.H, tile = (i * G + h % G) / plan.rows;
+            const Span span = span_of(a, s, G, tile * plan.rows,
+                                      min(s.n * G, (tile + 1) * plan.rows) - 1, plan.grain);
+            keys = part_keys(plan, span.len);
+            if (span.len <= keys) continue;
+            parts = (span.len + keys - 1) / keys;
+        }
         const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
         const float *sum = plan.part_sum + at * plan.parts, *ref = plan.part_ref + at * plan.parts;
         float top = -INFINITY;
@@ -362,10 +398,17 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int G = a.q_heads / c.H;
     const int span = c.width * c.page;
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
-    const int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
+    int most_kv = a.max_kv > 0 && a.max_kv < span ? a.max_kv : span;
     Shape r = {};
     const int64_t rows = int64_t(most_new) * G;
     r.rows = rows <= 16 ? 16 : c.dtype == SPARSP_F32 || (rows <= 32 && c.d <= 64) ? 32 : 128;
+    r.plan.rows = r.rows;
+    r.plan.grain = r.rows == 128 ? 64 : c.dtype == SPARSP_F32 ? 16 : 32;
+    if (a.window) {  // (the most that a tile's Span is long)
+        const int64_t tokens = std::min<int64_t>(most_new, r.rows / G + 2);
+        const int64_t seen = int64_t(a.sinks) + a.window + tokens + 2 * r.plan.grain;
+        most_kv = int(std::min<int64_t>(most_kv, seen));
+    }
     int64_t tiles = (rows + r.rows - 1) / r.rows;
     const int64_t pairs = int64_t(c.B) * c.H;
     // (a grid holds fewer than 2^32 threads, and units are rounded up to the eight XCDs)
@@ -412,7 +455,10 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
 
 template <typename T, int D, int NC>
 hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
-    paged_rows_kernel<T, D, NC><<<workgroups(p, a.cache), 256, 0, s>>>(a, p);
+    if (a.window)
+        paged_rows_kernel<T, D, NC, true><<<workgroups(p, a.cache), 256, 0, s>>>(a, p);
+    else
+        paged_rows_kernel<T, D, NC, false><<<workgroups(p, a.cache), 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
@@ -449,10 +495,11 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
     const bool shared = pairs * most_new <= 16 * kCus;
     const int64_t runs = shared ? most_new : (most_new + 7) / 8;  // workgroups of a head
     const int per = int(std::min(runs, std::max<int64_t>(1, (int64_t(1) << 15) / pairs)));
-    if (shared)
-        paged_merge_kernel<true><<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
-    else
-        paged_merge_kernel<false><<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
+    const auto merge = a.window ? (shared ? paged_merge_kernel<true, true>
+                                          : paged_merge_kernel<false, true>)
+                                : (shared ? paged_merge_kernel<true, false>
+                                          : paged_merge_kernel<false, false>);
+    merge<<<int(pairs) * per, 256, 0, s>>>(a, r.plan, per);
     return hipGetLastError();
 }
 

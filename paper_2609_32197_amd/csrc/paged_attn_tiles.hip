@@ -88,7 +88,7 @@ __device__ __forceinline__ void copy_rows(const u32x4_t& desc, const int (&off)[
 
 // D: channels of a row in LDS; those from C on are zero and left out of the products (d = 96,
 // 32 heads, 675 tokens over 24,153: 283 us, with all 128 328 us).
-template <int D, int C>
+template <int D, int C, bool WINDOW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     constexpr int TILE = kKeys * D;
@@ -109,12 +109,14 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
-    const int keys = part_keys(plan, s.kv);
-    const bool whole = s.kv <= keys;
-    if (part > 0 && part * int64_t(keys) >= s.kv) return;
-    const int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
+    Span span = {0, 0, s.kv, 0};
+    int keys = part_keys(plan, s.kv);
+    bool whole = s.kv <= keys;
+    if (!WINDOW && part > 0 && part * int64_t(keys) >= s.kv) return;
+    int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
     const float c2 = a.scale * kLog2e;
     const int shift = __builtin_ctz(c.page);
+    const int list_shift = WINDOW ? 4 : shift;  // (a window's gap is no multiple of a page)
     const uint32_t row_bytes = uint32_t(c.d) * 2, page_bytes = uint32_t(c.H * c.page) * row_bytes;
     // (48-bit addresses: the upper 16 bits of a descriptor's address word stay clear)
     const uint64_t head_at = uint64_t(uint32_t(hk * c.page)) * row_bytes;
@@ -146,14 +148,28 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     for (int turns = work.tile; turns * int64_t(kRowsTile) < rows; turns += work.stride) {
         const int n_tiles = (rows + kRowsTile - 1) / kRowsTile;
         const int tile = n_tiles - 1 - turns;
+        if constexpr (WINDOW) {
+            span = span_of(a, s, G, tile * kRowsTile, min(rows, (tile + 1) * kRowsTile) - 1, kKeys);
+            keys = part_keys(plan, span.len);
+            whole = span.len <= keys;
+            if (part > 0 && part * int64_t(keys) >= span.len) continue;
+            lo = part * keys;
+            part_end = min(span.len - lo, keys) + lo;
+        }
         bf16x8 q[2][KT];
         int limit[2], lowest = 1 << 30, highest = 0;
+        int earliest = 1 << 30, latest = 0;  // of the rows' windows, where they begin
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int r = tile * kRowsTile + wave * 32 + n * 16 + col;
             const bool live = r < rows;
             const int i = live ? r / G : 0, h = hk * G + (live ? r % G : 0);
             limit[n] = !live ? 0 : a.causal ? min(s.kv, s.kv - s.n + i + 1) : s.kv;
+            if (WINDOW && live) {
+                limit[n] -= span.skip;
+                earliest = min(earliest, limit[n] - a.window);
+                latest = max(latest, limit[n] - a.window);
+            }
             if (live) lowest = min(lowest, limit[n]);
             highest = max(highest, limit[n]);
             const uint16_t* p = static_cast<const uint16_t*>(a.Q) + int64_t(h) * a.q_head +
@@ -170,11 +186,20 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
         for (int off = 1; off < 16; off <<= 1) {
             lowest = min(lowest, __shfl_xor(lowest, off));
             highest = max(highest, __shfl_xor(highest, off));
+            if constexpr (WINDOW) {
+                earliest = min(earliest, __shfl_xor(earliest, off));
+                latest = max(latest, __shfl_xor(latest, off));
+            }
+        }
+        if constexpr (WINDOW) {
+            earliest = __builtin_amdgcn_readfirstlane(earliest);
+            latest = __builtin_amdgcn_readfirstlane(latest);
         }
         lowest = __builtin_amdgcn_readfirstlane(min(lowest, part_end));
         highest = __builtin_amdgcn_readfirstlane(min(highest, part_end));
         const int last = min(rows, (tile + 1) * kRowsTile) - 1;
-        const int end = min(a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv, part_end);
+        const int end =
+            min((a.causal ? min(s.kv, s.kv - s.n + last / G + 1) : s.kv) - span.skip, part_end);
 
         // l: sum of exponentials. lim: what a lane's eight may sum to before the reference moves;
         // kSeen, or -1: the row has seen nothing yet, or kFar. base: minus the reference in log2
@@ -191,24 +216,29 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
         }
 
         for (int seg = lo; seg < end; seg += kSegment) {
-            const int seg_end = min(end, seg + kSegment), p0 = seg >> shift;
+            const int seg_end = min(end, seg + kSegment), p0 = seg >> list_shift;
             __syncthreads();  // the list and the tiles of the segment before have been read
             int bad = 0;
-            for (int e = tid; e < ((((seg_end + kKeys - 1) & -kKeys) - 1) >> shift) - p0 + 1;
+            for (int e = tid; e < ((((seg_end + kKeys - 1) & -kKeys) - 1) >> list_shift) - p0 + 1;
                  e += 256) {
-                const int p = page_of(c.table, c.width, c.pages, b, p0 + e);
+                const int key = (p0 + e) << list_shift;
+                const bool seen = !WINDOW || span.sees(key, a.sinks);
+                const int p = seen ? page_of(c.table, c.width, c.pages, b,
+                                             WINDOW ? span.cached(key) >> shift : p0 + e)
+                                   : -1;
                 page_list[e] = p;
-                bad |= p < 0 && (p0 + e) << shift < seg_end;
+                bad |= p < 0 && seen && key < seg_end;
             }
             bad = __syncthreads_or(bad);
 
             auto issue = [&](int t0, auto buf_c) {
                 constexpr int buf = decltype(buf_c)::value;
                 const int key = t0 + 16 * wave;
-                const int p = __builtin_amdgcn_readfirstlane(page_list[(key >> shift) - p0]);
-                const int live = p < 0 ? 0 : min(max(s.kv - key, 0), 16);
+                const int p = __builtin_amdgcn_readfirstlane(page_list[(key >> list_shift) - p0]);
+                const int token = WINDOW ? span.cached(key) : key;
+                const int live = p < 0 ? 0 : min(max(s.kv - token, 0), 16);
                 const uint64_t at = uint64_t(uint32_t(max(p, 0))) * page_bytes +
-                                    uint32_t(key & (c.page - 1)) * row_bytes;
+                                    uint32_t(token & (c.page - 1)) * row_bytes;
                 u32x4_t desc;
                 desc.z = __builtin_amdgcn_readfirstlane(uint32_t(live) * row_bytes);
                 desc.w = 0x00020000u;
@@ -228,6 +258,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 __syncthreads();
                 if (t0 + kKeys < seg_end) issue(t0 + kKeys, std::integral_constant<int, buf ^ 1>{});
                 if (t0 >= highest) return;  // no row of this wave sees any of it
+                if (WINDOW && t0 + kKeys <= earliest && t0 >= a.sinks) return;
 
                 const char* lk = reinterpret_cast<const char*>(&lds[buf][0][0]);
                 const char* lv = reinterpret_cast<const char*>(&lds[buf][1][0]);
@@ -273,16 +304,18 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 v_operands(0);
                 __builtin_amdgcn_sched_barrier(0);
 
-                if (bad || t0 + kKeys > lowest) {
+                if (bad || t0 + kKeys > lowest ||
+                    (WINDOW && t0 < latest && t0 + kKeys > a.sinks)) {
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt) {
                         const int key = t0 + 32 * (mt >> 1) + 8 * g + 4 * (mt & 1);
-                        const bool gone = bad && page_list[(key >> shift) - p0] < 0;
+                        const bool gone = bad && page_list[(key >> list_shift) - p0] < 0;
 #pragma unroll
                         for (int n = 0; n < 2; ++n)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (gone || key + e >= min(limit[n], part_end))
+                                if (gone || key + e >= min(limit[n], part_end) ||
+                                    (WINDOW && key + e < limit[n] - a.window && key + e >= a.sinks))
                                     sc[n][mt][e] = -INFINITY;
                     }
                 }
@@ -421,13 +454,14 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
 }  // namespace
 
 hipError_t launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
-    const int grid = workgroups(p, a.cache);
-    if (a.cache.d <= 64)
-        paged_tiles_kernel<64, 64><<<grid, 256, 0, s>>>(a, p);
-    else if (a.cache.d <= 96)
-        paged_tiles_kernel<128, 96><<<grid, 256, 0, s>>>(a, p);
-    else
-        paged_tiles_kernel<128, 128><<<grid, 256, 0, s>>>(a, p);
+    const int grid = workgroups(p, a.cache), d = a.cache.d;
+    const auto kernel = a.window ? (d <= 64   ? paged_tiles_kernel<64, 64, true>
+                                    : d <= 96 ? paged_tiles_kernel<128, 96, true>
+                                              : paged_tiles_kernel<128, 128, true>)
+                                 : (d <= 64   ? paged_tiles_kernel<64, 64, false>
+                                    : d <= 96 ? paged_tiles_kernel<128, 96, false>
+                                              : paged_tiles_kernel<128, 128, false>);
+    kernel<<<grid, 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 

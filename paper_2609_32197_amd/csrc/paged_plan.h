@@ -10,6 +10,7 @@ namespace sparsp {
 // tiles of all sequences at most, a workgroup finds its own among them instead.
 struct PagedPlan {
     int tiles, parts, step, flat;
+    int rows, grain;  // rows of a tile; with a window, what its bounds are rounded to
     float* part_o;  // [q_heads, tokens, parts, d], normalised
     // A part's sum of exponentials [q_heads, tokens, parts], and behind all of them the score, not
     // yet scaled, that they are relative to (-inf: the part has nothing). Not the log of one times
@@ -124,6 +125,31 @@ __device__ __forceinline__ int part_keys(const PagedPlan& p, int kv) {
     const int64_t all = (int64_t(kv) + p.parts - 1) / p.parts;
     const int64_t k = (all + p.step - 1) / p.step * p.step;
     return int(k < p.step ? p.step : k);
+}
+
+// With a window the keys that some row of a tile sees are the first `head` cached tokens and, `skip`
+// behind them, those from the first row's window on: the tile walks `len` keys without the gap
+// between, key v of which is the cached token v + (v < head ? 0 : skip). Both bounds are multiples of
+// `grain`, so that no tile of `grain` keys lies across the gap. Limits of rows are shifted by skip
+// alike, which leaves every comparison of a key behind the gap with them as it was; before the gap
+// every row sees the first `sinks` tokens and no other.
+struct Span {
+    int head, skip, len, from;  // from: the key at which the first row's window begins
+    __device__ __forceinline__ int cached(int v) const { return v + (v < head ? 0 : skip); }
+    // Whether some row can see any of the 16 keys from v on, which lie on one page. The page of
+    // others may be anyone's by now.
+    __device__ __forceinline__ bool sees(int v, int sinks) const {
+        return v < sinks || v + 15 >= from;
+    }
+};
+// Of the rows [r0, r1] (token x group).
+__device__ __forceinline__ Span span_of(const PagedArgs& a, const Seq& s, int G, int r0, int r1,
+                                        int grain) {
+    const int first = s.kv - s.n + r0 / G + 1, last = s.kv - s.n + r1 / G + 1;
+    const int start = max(first - a.window, 0) & -grain;
+    const int head = min((a.sinks + grain - 1) & -grain, start);
+    const int skip = start - head;
+    return {head, skip, max(min(last, s.kv), 0) - skip, first - a.window - skip};
 }
 
 __device__ __forceinline__ void store4(void* O, int64_t at, bool bf16, const float (&x)[4]) {

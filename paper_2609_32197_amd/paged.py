@@ -61,11 +61,15 @@ _SIGNATURES.update({
     "sparsp_paged_attn": [_STRUCT, _I32, _STRUCT, _STRUCT, _I32, _VP, _I32, _F32, _I32, _I32, _VP,
                           _I64, _VP],
     "sparsp_paged_attn_workspace_bytes": [_STRUCT, _I32, _I32, _I32, _I32],
+    "sparsp_paged_attn_window": [_STRUCT, _I32, _STRUCT, _STRUCT, _I32, _VP, _I32, _I32, _F32, _I32,
+                                 _I32, _VP, _I64, _VP],
+    "sparsp_paged_attn_window_workspace_bytes": [_STRUCT, _I32, _I32, _I32, _I32, _I32, _I32],
     "sparsp_paged_weights": [_STRUCT, _I32, _STRUCT, _VP, _I32, _F32, _I32, _I32, _I32, _VP],
     "sparsp_cache_evict": [_STRUCT, _I32, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I64, _VP],
     "sparsp_cache_evict_workspace_bytes": [_STRUCT],
 })
 _RESTYPES["sparsp_paged_attn_workspace_bytes"] = _I64
+_RESTYPES["sparsp_paged_attn_window_workspace_bytes"] = _I64
 _RESTYPES["sparsp_cache_evict_workspace_bytes"] = _I64
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -311,15 +315,28 @@ def sparsp_paged_append(K, V, K_cache, V_cache, page_table, new_off, kv_len, wei
 
 
 def sparsp_paged_attn_workspace_bytes(K_cache, page_table, tokens: int, q_heads: int,
-                                      max_new: int = 0, max_kv: int = 0) -> int:
+                                      max_new: int = 0, max_kv: int = 0,
+                                      window: Optional[int] = None, sinks: int = 0) -> int:
     """Workspace bytes that sparsp_paged_attn can use for these shapes (host)."""
     B, width = page_table.shape
     P, H, page, d = K_cache.shape
     c = _CACHE.pack(0, 0, 0, 0, 0, 0, P, H, page, d, _dtype_code(K_cache, "K_cache"), width, B, 0)
-    n = int(load_library().sparsp_paged_attn_workspace_bytes(
-        c, _int(tokens, "tokens"), _int(q_heads, "q_heads"), *_hints(max_new, max_kv)))
+    c = (c, _int(tokens, "tokens"), _int(q_heads, "q_heads"))
+    if window is None and not sinks:
+        n = load_library().sparsp_paged_attn_workspace_bytes(*c, *_hints(max_new, max_kv))
+    else:
+        n = load_library().sparsp_paged_attn_window_workspace_bytes(
+            *c, *_window(window, sinks, True), *_hints(max_new, max_kv))
+    n = int(n)
     _check(n if n < 0 else 0)
     return n
+
+
+def _window(window, sinks, causal):
+    if window is None or not causal:
+        raise ValueError("sinks need a window" if window is None else
+                         "a window needs causal attention")
+    return _int(window, "window"), _int(sinks, "sinks")
 
 
 def _scale(softmax_scale, d):
@@ -329,13 +346,17 @@ def _scale(softmax_scale, d):
 def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: bool = True,
                       softmax_scale: Optional[float] = None, max_new: Optional[int] = None,
                       max_kv: Optional[int] = None, O=None, lse=None, want_lse: bool = True,
-                      out_dtype: Optional[int] = None, workspace=None, stream=None):
+                      out_dtype: Optional[int] = None, workspace=None, stream=None,
+                      window: Optional[int] = None, sinks: int = 0):
     """Attention of the new tokens Q [heads, tokens, d] over the cache. Returns (O, lse or None).
 
     O is [heads, tokens, d] (contiguous unless given), lse float32 [heads, tokens]. max_new and
     max_kv, the largest numbers of new and of cached tokens if the caller knows them, size the
     launch. With workspace (any device tensor, e.g. of sparsp_paged_attn_workspace_bytes bytes)
     long caches are split among workgroups; without, one workgroup walks a sequence's keys.
+
+    window: a token sees itself and the window - 1 tokens before it, and the sequence's first
+    `sinks` ones. Pages that no row sees are not read; their table entries may name no page.
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, None, page_table, new_off, kv_len)
@@ -354,10 +375,14 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     if workspace is not None:
         ws = _on(workspace, "workspace", dev)
         nbytes = workspace.numel() * workspace.element_size()
-    _call(load_library().sparsp_paged_attn, dev, stream, c, n, _rows(Q, "Q", dev, dt, n, d),
+    if window is None and not sinks:
+        fn, seen = load_library().sparsp_paged_attn, (bool(causal),)
+    else:
+        fn, seen = load_library().sparsp_paged_attn_window, _window(window, sinks, causal)
+    _call(fn, dev, stream, c, n, _rows(Q, "Q", dev, dt, n, d),
           _rows(o, "O", dev, odt, n, d, heads), _int(out_dtype, "out_dtype"),
           None if ls is None else _on(ls, "lse", dev, torch.float32, (heads, n)),
-          bool(causal), _scale(softmax_scale, d), *_hints(max_new, max_kv), ws, nbytes)
+          *seen, _scale(softmax_scale, d), *_hints(max_new, max_kv), ws, nbytes)
     return o, ls
 
 
