@@ -1,6 +1,11 @@
 /*
  * sparsp_bounded.h - C ABI of libsparsp for a paged cache (sparsp_cache.h) that is kept bounded: a
- * sliding window bounds what a token reads of it.
+ * sliding window bounds what a token reads of it, and 4 bits a value what it weighs.
+ *
+ *   sparsp_paged_attn_window  attention over the latest tokens and a few first ones
+ *   sparsp_paged_append4      new tokens' K and V into a cache of 4-bit values, K (and Q) rotated
+ *   sparsp_paged_attn4        attention over such a cache, with or without a window
+ *   sparsp_paged_read4        what such a cache holds of its latest tokens, back as rows
  *
  * The conventions of sparsp.h and sparsp_cache.h hold.
  */
@@ -29,6 +34,66 @@ int sparsp_paged_attn_window(const sparsp_cache* cache, int32_t tokens, const sp
 int64_t sparsp_paged_attn_window_workspace_bytes(const sparsp_cache* cache, int32_t tokens,
                                                  int32_t q_heads, int32_t window, int32_t sinks,
                                                  int32_t max_new, int32_t max_kv);
+
+/*
+ * A cache held in 4 bits. A code is sign (bit 3) and magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0-2);
+ * 32 channels of a token share a scale byte s, and a code stands for its value times 2^(s - 127), or
+ * for NaN where s is 255. Codes lie as [pages, H, page, d / 2], channel 2c in the low and 2c + 1 in
+ * the high half of byte c; scales as [pages, H, d / 32, page], so a token's scales lie `page` bytes
+ * apart. Page for page, codes and scales can be copied and shared like K and V of sparsp_cache. 4.25
+ * bits a value. d is a multiple of 32 up to 128; the rest as for sparsp_cache.
+ */
+typedef struct {
+    uint8_t *K, *K_scales, *V, *V_scales;
+    const int32_t* table;   /* [B, width] page numbers */
+    const int32_t* new_off; /* [B + 1] */
+    const int32_t* kv_len;  /* [B] */
+    int32_t pages, H, page, d, width, B;
+    int32_t reserved[2]; /* 0 */
+} sparsp_cache4;
+
+/*
+ * sparsp_paged_append into such a cache; rows K, V, Q and Q_out are of `dtype`. With a the largest
+ * magnitude of a token's 32 channels their scale is 2^e, e = floor(log2 a) - 2 but at least -125
+ * and at most 125; a code is the nearest one to the value over 2^e, of two as near the one with an
+ * even code, and 6 for what is larger than 6. (So a value is off by a fifth of itself at most, or a
+ * quarter where it is above 7 times the scale, or by a quarter of the scale where it is below half of
+ * it.) 32 channels with an infinity or a NaN become NaN. The rotation of K is computed in 64 bits and
+ * not rounded before that, so that codes do not depend on the rounding of a product; Q is rotated in
+ * float32, as by sparsp_rope.
+ */
+int sparsp_paged_append4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype,
+                         const sparsp_rows* K, const sparsp_rows* V, const sparsp_rotary* r,
+                         const void* positions, int32_t position_bits, const float* inv_freq,
+                         const sparsp_rows* Q, const sparsp_rows* Q_out, void* stream);
+
+/*
+ * sparsp_paged_attn over what the codes stand for; Q is of `dtype`, O of out_dtype (F32 always; BF16
+ * where dtype is BF16). window 0: every cached token is visible as there; window > 0 (with causal
+ * only): as in sparsp_paged_attn_window. What the codes stand for is exact in bf16, and products run
+ * on the bf16 matrix cores with float32 sums. bf16 rows: precision as in sparsp_paged_attn. float32
+ * rows, and their probabilities, enter the products as three bf16 each, that is to 2^-24 of themselves.
+ * Q must be finite, and no scale of 255 may lie among the tokens of a page that some row sees.
+ */
+int sparsp_paged_attn4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype,
+                       const sparsp_rows* Q, const sparsp_rows* O, int32_t out_dtype, float* lse,
+                       int32_t causal, int32_t window, int32_t sinks, float softmax_scale,
+                       int32_t max_new, int32_t max_kv, void* workspace, int64_t workspace_bytes,
+                       void* stream);
+
+/* Workspace bytes that sparsp_paged_attn4 can use (>= 0), or a negative status. Host only. */
+int64_t sparsp_paged_attn4_workspace_bytes(const sparsp_cache4* cache, int32_t tokens, int32_t dtype,
+                                           int32_t q_heads, int32_t window, int32_t sinks,
+                                           int32_t max_new, int32_t max_kv);
+
+/*
+ * K and V [H, tokens, d] of `dtype` become what the cache holds of the new tokens (exact in either
+ * type). With new_off as the running sums of kv_len that is the whole cache, token after token. A
+ * token whose place has no page, or lies before the first cached one, reads as 0; columns of no
+ * sequence stay as they are.
+ */
+int sparsp_paged_read4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype,
+                       const sparsp_rows* K, const sparsp_rows* V, void* stream);
 
 #ifdef __cplusplus
 }

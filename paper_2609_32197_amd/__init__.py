@@ -40,6 +40,13 @@ A growing sequence and its paged cache (paged.py, include/sparsp_cache.h):
     sparsp_paged_weights           attention weight per cached token
     sparsp_cache_evict             the cache cut to the tokens of most weight
 
+The cache kept bounded (bounded.py, include/sparsp_bounded.h):
+
+    sparsp_paged_attn(window=)     attention over the latest tokens and a few first ones
+    sparsp_paged_append4           new tokens into a cache of 4-bit values
+    sparsp_paged_attn4             attention over such a cache
+    sparsp_paged_read4             what such a cache holds, back as rows
+
 Calls run on the current stream, or on `stream` where one is given. Outputs that a call makes itself
 come from the memory of that stream: wait for it before they are used on another.
 
@@ -737,5 +744,7 @@ route_volume = sparsp_route_volume
 
 from . import paged as _paged  # noqa: E402  (it uses the helpers above)
 from .paged import *  # noqa: E402,F401,F403
+from . import bounded as _bounded  # noqa: E402
+from .bounded import *  # noqa: E402,F401,F403
 
-__all__ += _paged.__all__
+__all__ += _paged.__all__ + _bounded.__all__

@@ -36,27 +36,12 @@ int attn(const sparsp_cache* cache, int tokens, const sparsp_rows* Q, const spar
     sparsp::PagedArgs a;
     if (int rc = check_query(cache, tokens, Q, softmax_scale, max_new, max_kv, &a)) return rc;
     if (int rc = check_pointers(cache, true, false, true)) return rc;
-    if (out_dtype != SPARSP_F32 && out_dtype != SPARSP_BF16)
-        return fail(SPARSP_E_DTYPE, "unknown out_dtype %d", out_dtype);
-    if (cache->dtype == SPARSP_F32 && out_dtype != SPARSP_F32)
-        return fail(SPARSP_E_DTYPE, "f32 inputs produce f32 output only");
-    if (int rc = check_rows(O, "O", tokens, cache->d, out_dtype == SPARSP_BF16 ? 2 : 4, true)) return rc;
-    if (O->heads != Q->heads)
-        return fail(SPARSP_E_INVALID, "O has %d heads, Q has %d", O->heads, Q->heads);
-    if (O->data == Q->data) return fail(SPARSP_E_INVALID, "O may not be Q");
-    if (workspace_bytes < 0) return fail(SPARSP_E_INVALID, "workspace_bytes < 0");
-    if (!aligned16(workspace)) return fail(SPARSP_E_INVALID, "workspace must be 16-byte aligned");
+    if (int rc = check_output(tokens, Q, O, out_dtype, workspace, workspace_bytes, &a)) return rc;
     if (tokens == 0) return ok();
     a.causal = causal;
     a.window = window < kFarthest ? window : kFarthest;
     a.sinks = sinks < kFarthest ? sinks : kFarthest;
-    a.O = O->data;
-    a.o_head = O->head_stride;
-    a.o_token = O->token_stride;
-    a.out_bf16 = out_dtype == SPARSP_BF16;
     a.lse = lse;
-    a.ws = workspace;
-    a.ws_bytes = workspace ? workspace_bytes : 0;
     return hip_status(sparsp::launch_paged_attn(a, (hipStream_t)stream), name);
 }
 

@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t kMaxPairs = int64_t(1) << 20;  // sequences x heads: workgroups of a launch
 
-int fail(int code, const char* fmt, ...) {
+inline int fail(int code, const char* fmt, ...) {
     char msg[400];
     va_list ap;
     va_start(ap, fmt);
@@ -22,16 +22,16 @@ int fail(int code, const char* fmt, ...) {
     return sparsp::set_error(code, msg);
 }
 
-int ok() { return sparsp::set_error(SPARSP_OK, ""); }
+inline int ok() { return sparsp::set_error(SPARSP_OK, ""); }
 
-int hip_status(hipError_t e, const char* what) {
+inline int hip_status(hipError_t e, const char* what) {
     if (e != hipSuccess) return fail(SPARSP_E_HIP, "%s: %s", what, hipGetErrorString(e));
     return ok();
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int check_type(int d, int dtype, int most) {
+inline int check_type(int d, int dtype, int most) {
     if (dtype != SPARSP_F32 && dtype != SPARSP_BF16)
         return fail(SPARSP_E_DTYPE, "unknown dtype %d", dtype);
     if (d <= 0) return fail(SPARSP_E_INVALID, "d = %d must be positive", d);
@@ -45,7 +45,7 @@ int check_type(int d, int dtype, int most) {
 // Whether two of a tensor's rows share a channel; both strides are d at least. Heads beside one
 // another behind all tokens, or tokens behind all heads, are seen at once; else the token that begins
 // next to each head's first decides.
-bool rows_overlap(const sparsp_rows* r, int tokens, int d) {
+inline bool rows_overlap(const sparsp_rows* r, int tokens, int d) {
     const int64_t hs = r->head_stride, ts = r->token_stride;
     if (r->heads < 2 || tokens < 2) return false;
     if ((hs - d) / ts >= tokens - 1 || (ts - d) / hs >= r->heads - 1) return false;
@@ -58,7 +58,7 @@ bool rows_overlap(const sparsp_rows* r, int tokens, int d) {
 }
 
 // A [heads, tokens, d] tensor of elements of `size` bytes.
-int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int size,
+inline int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int size,
                bool written = false) {
     if (!r || !r->data) return fail(SPARSP_E_INVALID, "%s is NULL", name);
     if (r->heads < 1 || r->heads > 1024)
@@ -75,7 +75,7 @@ int check_rows(const sparsp_rows* r, const char* name, int tokens, int d, int si
     return SPARSP_OK;
 }
 
-int check_cache(const sparsp_cache* c) {
+inline int check_cache(const sparsp_cache* c) {
     if (!c) return fail(SPARSP_E_INVALID, "cache is NULL");
     if (int rc = check_type(c->d, c->dtype, 128)) return rc;
     if (c->pages < 1 || c->width < 1 || c->B < 1)
@@ -95,7 +95,7 @@ int check_cache(const sparsp_cache* c) {
 }
 
 // The device arrays that a call reads.
-int check_pointers(const sparsp_cache* c, bool values, bool weights, bool batch) {
+inline int check_pointers(const sparsp_cache* c, bool values, bool weights, bool batch) {
     if (!c->K || (values && !c->V) || !c->table || !c->kv_len || (batch && !c->new_off))
         return fail(SPARSP_E_INVALID, "NULL cache pointer");
     if (!aligned16(c->K) || !aligned16(c->V))
@@ -105,19 +105,19 @@ int check_pointers(const sparsp_cache* c, bool values, bool weights, bool batch)
 }
 
 // For calls that write both.
-int check_apart(const sparsp_cache* c) {
+inline int check_apart(const sparsp_cache* c) {
     if (c->K == c->V) return fail(SPARSP_E_INVALID, "K and V of the cache are the same memory");
     return SPARSP_OK;
 }
 
-int check_tokens(int tokens) {
+inline int check_tokens(int tokens) {
     if (tokens < 0 || tokens > (1 << 26))
         return fail(SPARSP_E_INVALID, "tokens = %d outside [0, 2^26]", tokens);
     return SPARSP_OK;
 }
 
 // The rotation of rows of d channels, into a.
-int check_rotary(const sparsp_rotary* r, int d, const void* positions, int bits,
+inline int check_rotary(const sparsp_rotary* r, int d, const void* positions, int bits,
                  const float* inv_freq, sparsp::RotateArgs* a) {
     if (!r) return fail(SPARSP_E_INVALID, "the rotation is NULL");
     if (r->rot_dim < 2 || r->rot_dim > d || r->rot_dim % 2)
@@ -150,7 +150,7 @@ int check_rotary(const sparsp_rotary* r, int d, const void* positions, int bits,
     return SPARSP_OK;
 }
 
-sparsp::RowMove row_move(const sparsp_rows& x, const sparsp_rows& y, bool rotate) {
+inline sparsp::RowMove row_move(const sparsp_rows& x, const sparsp_rows& y, bool rotate) {
     sparsp::RowMove m;
     m.src = x.data;
     m.src_head = x.head_stride;
@@ -163,14 +163,14 @@ sparsp::RowMove row_move(const sparsp_rows& x, const sparsp_rows& y, bool rotate
     return m;
 }
 
-sparsp::RowMove page_move(const sparsp_rows& x, void* cache, bool rotate) {
+inline sparsp::RowMove page_move(const sparsp_rows& x, void* cache, bool rotate) {
     sparsp::RowMove m = row_move(x, x, rotate);
     m.dst = cache;
     m.paged = true;
     return m;
 }
 
-int check_same_rows(const sparsp_rows* x, const sparsp_rows* y, const char* name) {
+inline int check_same_rows(const sparsp_rows* x, const sparsp_rows* y, const char* name) {
     if (x->heads != y->heads)
         return fail(SPARSP_E_INVALID, "%s: input and output have %d and %d heads", name, x->heads,
                     y->heads);
@@ -181,7 +181,7 @@ int check_same_rows(const sparsp_rows* x, const sparsp_rows* y, const char* name
 }
 
 // What attention and weights share.
-int check_query(const sparsp_cache* c, int tokens, const sparsp_rows* Q, float scale, int max_new,
+inline int check_query(const sparsp_cache* c, int tokens, const sparsp_rows* Q, float scale, int max_new,
                 int max_kv, sparsp::PagedArgs* a) {
     if (int rc = check_cache(c)) return rc;
     if (int rc = check_tokens(tokens)) return rc;
@@ -205,6 +205,28 @@ int check_query(const sparsp_cache* c, int tokens, const sparsp_rows* Q, float s
     a->scale = scale;
     a->max_new = max_new;
     a->max_kv = max_kv;
+    return SPARSP_OK;
+}
+
+// An attention call's output and workspace, into a.
+inline int check_output(int tokens, const sparsp_rows* Q, const sparsp_rows* O, int out_dtype,
+                 void* workspace, int64_t workspace_bytes, sparsp::PagedArgs* a) {
+    if (out_dtype != SPARSP_F32 && out_dtype != SPARSP_BF16)
+        return fail(SPARSP_E_DTYPE, "unknown out_dtype %d", out_dtype);
+    if (a->cache.dtype == SPARSP_F32 && out_dtype != SPARSP_F32)
+        return fail(SPARSP_E_DTYPE, "f32 inputs produce f32 output only");
+    if (int rc = check_rows(O, "O", tokens, a->cache.d, out_dtype == SPARSP_BF16 ? 2 : 4, true)) return rc;
+    if (O->heads != Q->heads)
+        return fail(SPARSP_E_INVALID, "O has %d heads, Q has %d", O->heads, Q->heads);
+    if (O->data == Q->data) return fail(SPARSP_E_INVALID, "O may not be Q");
+    if (workspace_bytes < 0) return fail(SPARSP_E_INVALID, "workspace_bytes < 0");
+    if (!aligned16(workspace)) return fail(SPARSP_E_INVALID, "workspace must be 16-byte aligned");
+    a->O = O->data;
+    a->o_head = O->head_stride;
+    a->o_token = O->token_stride;
+    a->out_bf16 = out_dtype == SPARSP_BF16;
+    a->ws = workspace;
+    a->ws_bytes = workspace ? workspace_bytes : 0;
     return SPARSP_OK;
 }
 

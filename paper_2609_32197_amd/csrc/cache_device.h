@@ -26,6 +26,24 @@ __device__ __forceinline__ int page_of(const int32_t* table, int width, int page
     return p >= 0 && p < pages ? p : -1;
 }
 
+// The row of head 0 that token t's place is (rows of a page are numbered [H, page]), kNoPlace, or
+// kNoSequence for a column of no sequence, which nothing is written for. The lanes of a wave
+// together: new_off is ascending, so the token's sequence is the number of ends new_off[1..B] at or
+// before it, counted 64 at a time.
+constexpr int64_t kNoPlace = -1, kNoSequence = -2;
+__device__ __forceinline__ int64_t place_of(const sparsp_cache& c, int tokens, int t, int lane) {
+    int b = 0;
+    for (int e = lane; e < c.B; e += 64) b += c.new_off[e + 1] <= t;
+    for (int off = 32; off; off >>= 1) b += __shfl_xor(b, off);
+    if (b >= c.B) return kNoSequence;
+    const Seq s = sequence(c, tokens, b);
+    const int i = t - s.q0, slot = s.kv - s.n + i;
+    if (i < 0 || i >= s.n) return kNoSequence;
+    if (slot < 0) return kNoPlace;
+    const int page = page_of(c.table, c.width, c.pages, b, slot >> __builtin_ctz(c.page));
+    return page < 0 ? kNoPlace : int64_t(page) * c.H * c.page + (slot & (c.page - 1));
+}
+
 // x / d for 0 <= x < 2^31 by one multiplication: m = floor(2^32 / d) + 1 is exact while
 // x * d < 2^32; a step corrects larger x.
 struct Div {

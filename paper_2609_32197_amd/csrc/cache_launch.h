@@ -41,8 +41,19 @@ struct RotateArgs {
 };
 hipError_t launch_rotate_rows(const RotateArgs& a, hipStream_t s);
 
+// New tokens into a cache held in 4 bits, and what it holds of them back. cache.K and cache.V are
+// codes, cache.dtype is the rows'.
+struct FourArgs {
+    RotateArgs rows;  // move[0]: K, move[1]: V; move[2]: Q
+    uint8_t *k_scales = nullptr, *v_scales = nullptr;
+};
+hipError_t launch_four_append(const FourArgs& a, hipStream_t s);
+hipError_t launch_four_read(const FourArgs& a, hipStream_t s);
+
 struct PagedArgs {
     sparsp_cache cache;
+    // Of a cache held in 4 bits, whose K and V are codes and whose dtype is that of the rows; or NULL.
+    const uint8_t *k_scales, *v_scales;
     int tokens, q_heads;
     const void* Q;
     int64_t q_head, q_token;

@@ -1,0 +1,366 @@
+// New tokens into a cache held in 4 bits, and back (the format is stated in paged_four.h).
+//
+// With a the largest magnitude of 32 channels the scale is 2^e, e = floor(log2 a) - 2, so that every
+// magnitude is below 8 of it; a code is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even one,
+// 6 for what is larger. All that is exact: e comes from the exponents' bits alone, and a magnitude is
+// rounded once, by rint of a multiple of a power of two.
+//
+// K is rotated on the way in 64 bits. A code jumps by a third of its value where a value crosses a
+// border, so that with 32 bits it would depend, once in some 10^6 values, on the rounding of a
+// product; in 64 bits a value is as near to a border once in 10^10. Q, which stays in its own type,
+// is rotated in float32 as by sparsp_rope.
+//
+// A thread takes eight channels, a dword of codes; four neighbours share a scale. A workgroup takes
+// `per` tokens and shares their cosines and sines over all heads, as in rotate_rows.hip.
+#include "cache_device.h"
+#include "paged_four.h"
+
+namespace sparsp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxPer = 16;        // tokens of a workgroup at most
+constexpr int kTablePairs = 1024;  // cosines and sines held
+
+struct Side {
+    const char* src;
+    int64_t head, token;  // bytes
+    uint8_t *codes, *scales;
+};
+struct Params {
+    Side kv[2];
+    const char* q;
+    char* q_out;
+    int64_t q_head, q_token, out_head, out_token;
+    int q_heads;
+    int tokens, P, inverse, wide;
+    Div per, units, q_units, q_heads_div, heads;
+    int axis_end[3];
+    float factor;
+    const void* positions;
+    const float* inv_freq;
+    sparsp_cache cache;
+};
+
+template <typename T>
+__device__ __forceinline__ float up(T x);
+template <>
+__device__ __forceinline__ float up<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float up<uint16_t>(uint16_t x) { return bf16_bits_to_f32(x); }
+template <typename T>
+__device__ __forceinline__ T down(float x);
+template <>
+__device__ __forceinline__ float down<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ uint16_t down<uint16_t>(float x) { return uint16_t(f32_to_bf16_bits(x)); }
+
+template <typename T, int V>
+struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec {
+    T e[V];
+};
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> get(const char* row, int ch) {
+    return *reinterpret_cast<const Vec<T, V>*>(row + ch * int(sizeof(T)));
+}
+
+// Codes of eight channels and the scale's exponent byte, which the four lanes of a group share.
+__device__ __forceinline__ uint32_t magnitude(double y) {  // grows with |y|; its exponent from bit 20
+    return uint32_t(__double2hiint(y)) & 0x7fffffffu;
+}
+template <typename Y>
+__device__ __forceinline__ uint32_t quantise(const Y (&y)[8], uint32_t* scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, magnitude(double(y[e])));
+    top = max(top, uint32_t(__shfl_xor(int(top), 1)));
+    top = max(top, uint32_t(__shfl_xor(int(top), 2)));
+    if (top >= 0x7ff00000u) {  // an infinity or a NaN: the scale that stands for NaN
+        *scale = 255;
+        return 0;
+    }
+    const int exponent = min(max(int(top >> 20) - 1023 - 2, -125), 125);
+    *scale = uint32_t(exponent + 127);
+    const Y unit = Y(__uint_as_float(uint32_t(127 - exponent) << 23));
+    uint32_t codes = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const Y a = y[e] < 0 ? -y[e] : y[e], m = a * unit;
+        // Steps of a half below 2, of one below 4, of two from there.
+        const Y step = m < 2 ? Y(2) : m < 4 ? Y(1) : Y(0.5);
+        const int base = m < 2 ? 0 : m < 4 ? 2 : 4;
+        const int code = min(int(rint(m * step)) + base, 7);
+        const bool sign = sizeof(Y) == 8 ? __double2hiint(double(y[e])) < 0
+                                         : int(__float_as_uint(float(y[e]))) < 0;
+        codes |= uint32_t(code | (sign ? 8 : 0)) << (4 * e);
+    }
+    return codes;
+}
+
+template <typename T, int V, bool HALF>
+__global__ __launch_bounds__(kThreads) void four_append_kernel(const Params p) {
+    __shared__ double2 turn[kTablePairs];
+    __shared__ int64_t place[kMaxPer];
+    const sparsp_cache& c = p.cache;
+    const int t0 = blockIdx.x * p.per.d, count = min(int(p.per.d), p.tokens - t0);
+    const int lane = threadIdx.x & 63;
+    for (int k = threadIdx.x >> 6; k < count; k += kThreads / 64) {
+        const int64_t row = place_of(c, p.tokens, t0 + k, lane);
+        if (lane == 0) place[k] = row;
+    }
+    for (int e = threadIdx.x; e < count * p.P; e += kThreads) {
+        const int k = e / p.P, pr = e % p.P;
+        const int axis = (pr >= p.axis_end[0]) + (pr >= p.axis_end[1]);
+        const int64_t at = int64_t(axis) * p.tokens + t0 + k;
+        const double x = p.wide ? double(static_cast<const int64_t*>(p.positions)[at])
+                                : double(static_cast<const int32_t*>(p.positions)[at]);
+        constexpr double kInvTurn = 0.15915494309189533576888;  // 1 / (2 pi)
+        double r = x * double(p.inv_freq[pr]) * kInvTurn;
+        r -= rint(r);
+        double s, cs;
+        sincospi(2.0 * r, &s, &cs);
+        turn[e] = make_double2(cs * p.factor, (p.inverse ? -s : s) * p.factor);
+    }
+    __syncthreads();
+
+    // Q: units of V pairs, then of V channels that stay.
+    if (p.q) {
+        const uint32_t turned = HALF ? p.P / V : 2 * p.P / V;
+        const uint32_t items = uint32_t(count) * p.q_heads * p.q_units.d;
+        for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
+            const uint32_t row = p.q_units.quot(it), u = it - row * p.q_units.d;
+            const uint32_t k = p.q_heads_div.quot(row), h = row - k * p.q_heads;
+            if (place[k] == kNoSequence) continue;
+            const char* in = p.q + int64_t(h) * p.q_head + int64_t(t0 + k) * p.q_token;
+            char* out = p.q_out + int64_t(h) * p.out_head + int64_t(t0 + k) * p.out_token;
+            const double2* cs = turn + k * p.P;
+            auto put = [&](int ch, const Vec<T, V>& x) {
+                *reinterpret_cast<Vec<T, V>*>(out + ch * int(sizeof(T))) = x;
+            };
+            if (u >= turned) {
+                const int ch = int(u + (HALF ? turned : 0)) * V;
+                put(ch, get<T, V>(in, ch));
+            } else if (HALF) {
+                const int ch = int(u) * V;
+                const Vec<T, V> a = get<T, V>(in, ch), b = get<T, V>(in, ch + p.P);
+                Vec<T, V> ya, yb;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float tc = float(cs[ch + e].x), ts = float(cs[ch + e].y);
+                    const float x1 = up<T>(a.e[e]), x2 = up<T>(b.e[e]);
+                    ya.e[e] = down<T>(x1 * tc - x2 * ts);
+                    yb.e[e] = down<T>(x1 * ts + x2 * tc);
+                }
+                put(ch, ya);
+                put(ch + p.P, yb);
+            } else if constexpr (V >= 2) {
+                const int ch = int(u) * V;
+                const Vec<T, V> a = get<T, V>(in, ch);
+                Vec<T, V> y;
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const double2 t = cs[(ch + e) / 2];
+                    const float tc = float(t.x), ts = float(t.y);
+                    const float x1 = up<T>(a.e[e]), x2 = up<T>(a.e[e + 1]);
+                    y.e[e] = down<T>(x1 * tc - x2 * ts);
+                    y.e[e + 1] = down<T>(x1 * ts + x2 * tc);
+                }
+                put(ch, y);
+            }
+        }
+    }
+
+    // K and V: units of eight channels; a row's units fill whole groups of four lanes.
+    const uint32_t items = uint32_t(count) * c.H * p.units.d;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const Side& sd = p.kv[side];
+        for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
+            const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
+            const uint32_t k = p.heads.quot(row), h = row - k * c.H;
+            const int64_t at = place[k];
+            if (at < 0) continue;
+            const char* in = sd.src + int64_t(h) * sd.head + int64_t(t0 + k) * sd.token;
+            const int ch = int(u) * 8;
+            const Vec<T, 8> x = get<T, 8>(in, ch);
+            uint32_t scale, codes;
+            if (side == 0 && p.P > 0) {
+                const double2* cs = turn + k * p.P;
+                double y[8];
+                if (HALF) {
+#pragma unroll
+                    for (int e0 = 0; e0 < 8; e0 += V) {
+                        const int first = ch + e0, behind = first >= p.P;
+                        const bool turns = first < 2 * p.P;
+                        const Vec<T, V> other =
+                            get<T, V>(in, turns ? behind ? first - p.P : first + p.P : first);
+                        const double2* t = cs + (turns ? first - (behind ? p.P : 0) : 0);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const double own = double(up<T>(x.e[e0 + e])), far = double(up<T>(other.e[e]));
+                            const double sn = behind ? t[e].y : -t[e].y;
+                            y[e0 + e] = turns ? own * t[e].x + far * sn : own;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const bool turns = ch + e < 2 * p.P;
+                        const double2 t = cs[turns ? (ch + e) / 2 : 0];
+                        const double x1 = double(up<T>(x.e[e])), x2 = double(up<T>(x.e[e + 1]));
+                        y[e] = turns ? x1 * t.x - x2 * t.y : x1;
+                        y[e + 1] = turns ? x1 * t.y + x2 * t.x : x2;
+                    }
+                }
+                codes = quantise(y, &scale);
+            } else {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = up<T>(x.e[e]);
+                codes = quantise(y, &scale);
+            }
+            const int64_t to = at + int64_t(h) * c.page;  // (c.page a power of two, heads [page] rows)
+            *reinterpret_cast<uint32_t*>(sd.codes + to * (c.d / 2) + 4 * u) = codes;
+            if (u % 4 == 0) {
+                const int slot = int(to & (c.page - 1));
+                sd.scales[(to - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot] = uint8_t(scale);
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void four_read_kernel(const Params p) {
+    __shared__ int64_t place[kMaxPer];
+    const sparsp_cache& c = p.cache;
+    const int t0 = blockIdx.x * p.per.d, count = min(int(p.per.d), p.tokens - t0);
+    const int lane = threadIdx.x & 63;
+    for (int k = threadIdx.x >> 6; k < count; k += kThreads / 64) {
+        const int64_t row = place_of(c, p.tokens, t0 + k, lane);
+        if (lane == 0) place[k] = row;
+    }
+    __syncthreads();
+    const uint32_t items = uint32_t(count) * c.H * p.units.d;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const Side& sd = p.kv[side];
+        for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
+            const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
+            const uint32_t k = p.heads.quot(row), h = row - k * c.H;
+            const int64_t at = place[k];
+            if (at == kNoSequence) continue;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (at >= 0) {
+                const int64_t from = at + int64_t(h) * c.page;
+                const int slot = int(from & (c.page - 1));
+                const uint32_t codes =
+                    *reinterpret_cast<const uint32_t*>(sd.codes + from * (c.d / 2) + 4 * u);
+                const uint32_t scale =
+                    sd.scales[(from - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot];
+                x = four_octet(codes, __uint_as_float(scale << 23));
+            }
+            char* out = const_cast<char*>(sd.src) + int64_t(h) * sd.head + int64_t(t0 + k) * sd.token;
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint4*>(out + 16 * u) = x;
+            } else {
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint4 y;
+                    y.x = w[2 * e] << 16;
+                    y.y = w[2 * e] & 0xffff0000u;
+                    y.z = w[2 * e + 1] << 16;
+                    y.w = w[2 * e + 1] & 0xffff0000u;
+                    *reinterpret_cast<uint4*>(out + 32 * u + 16 * e) = y;
+                }
+            }
+        }
+    }
+}
+
+Params params(const FourArgs& f, int pairs) {
+    const RotateArgs& a = f.rows;
+    const int size = a.bf16 ? 2 : 4;
+    Params p = {};
+    for (int n = 0; n < 2; ++n)
+        p.kv[n] = {static_cast<const char*>(a.move[n].src), a.move[n].src_head * size,
+                   a.move[n].src_token * size,
+                   static_cast<uint8_t*>(n == 0 ? a.cache.K : a.cache.V),
+                   n == 0 ? f.k_scales : f.v_scales};
+    p.tokens = a.tokens;
+    p.P = pairs;
+    p.cache = a.cache;
+    p.units = make_div(uint32_t(a.cache.d / 8));
+    p.heads = make_div(uint32_t(a.cache.H));
+    // As in rotate_rows.hip: enough workgroups to fill the GPU four times, then longer runs.
+    int per = 1;
+    while (per < kMaxPer && a.tokens / (2 * per) >= 1024 &&
+           (pairs == 0 || 2 * per * pairs <= kTablePairs))
+        per *= 2;
+    p.per = make_div(uint32_t(per));
+    return p;
+}
+
+template <typename T, int V>
+void launch_append(const Params& p, bool half, hipStream_t s) {
+    const int grid = (p.tokens + int(p.per.d) - 1) / int(p.per.d);
+    if (half)
+        four_append_kernel<T, V, true><<<grid, kThreads, 0, s>>>(p);
+    else
+        four_append_kernel<T, V, false><<<grid, kThreads, 0, s>>>(p);
+}
+template <typename T>
+void launch_width(const Params& p, bool half, int width, hipStream_t s) {
+    if (width == 8) return launch_append<T, 8>(p, half, s);
+    if (width == 4) return launch_append<T, 4>(p, half, s);
+    if (width == 2) return launch_append<T, 2>(p, half, s);
+    launch_append<T, 1>(p, half, s);
+}
+
+}  // namespace
+
+hipError_t launch_four_append(const FourArgs& f, hipStream_t s) {
+    const RotateArgs& a = f.rows;
+    const int size = a.bf16 ? 2 : 4;
+    Params p = params(f, a.rot / 2);
+    p.inverse = a.inverse;
+    p.wide = a.wide;
+    for (int x = 0; x < 3; ++x) p.axis_end[x] = a.axis_end[x];
+    p.factor = a.factor;
+    p.positions = a.positions;
+    p.inv_freq = a.inv_freq;
+    const bool half = a.rot && a.layout == SPARSP_ROPE_HALF;
+    // The widest unit that divides the rotated part (its half, where a pair lies in two units).
+    const int part = half ? a.rot / 2 : a.rot;
+    int width = 8;
+    while (part % width) width /= 2;
+    if (a.moves == 3) {
+        const RowMove& q = a.move[2];
+        p.q = static_cast<const char*>(q.src);
+        p.q_out = static_cast<char*>(q.dst);
+        p.q_head = q.src_head * size;
+        p.q_token = q.src_token * size;
+        p.out_head = q.dst_head * size;
+        p.out_token = q.dst_token * size;
+        p.q_heads = q.heads;
+        p.q_heads_div = make_div(uint32_t(q.heads));
+        p.q_units = make_div(uint32_t((a.cache.d - (half ? a.rot / 2 : 0)) / width));
+    }
+    if (a.bf16)
+        launch_width<uint16_t>(p, half, width, s);
+    else
+        launch_width<float>(p, half, width, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_four_read(const FourArgs& f, hipStream_t s) {
+    const Params p = params(f, 0);
+    const int grid = (p.tokens + int(p.per.d) - 1) / int(p.per.d);
+    if (f.rows.bf16)
+        four_read_kernel<uint16_t><<<grid, kThreads, 0, s>>>(p);
+    else
+        four_read_kernel<float><<<grid, kThreads, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace sparsp

@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "paged_tiles.h"
+#include "paged_four.h"
 
 namespace sparsp {
 namespace {
@@ -105,11 +105,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
         };
         auto load_k = [&](Stage& st, int t0, int p0) {
             st.kp = page_list[((t0 + M::k_group(lane)) >> list_shift) - p0];
-            M::load_k(c, st.k, st.kp, hk, WINDOW ? span.cached(t0) : t0, lane);
+            M::load_k(M::source(a), st.k, st.kp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         auto load_v = [&](Stage& st, int t0, int p0) {
             st.vp = page_list[((t0 + M::v_group(lane)) >> list_shift) - p0];
-            M::load_v(c, st.v, st.vp, hk, WINDOW ? span.cached(t0) : t0, lane);
+            M::load_v(M::source(a), st.v, st.vp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         // after_scores: what is done once K has been used.
         auto compute = [&](Stage& st, int t0, auto after_scores) {
@@ -403,7 +403,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int64_t rows = int64_t(most_new) * G;
     r.rows = rows <= 16 ? 16 : c.dtype == SPARSP_F32 || (rows <= 32 && c.d <= 64) ? 32 : 128;
     r.plan.rows = r.rows;
-    r.plan.grain = r.rows == 128 ? 64 : c.dtype == SPARSP_F32 ? 16 : 32;
+    r.plan.grain = r.rows == 128 ? 64 : c.dtype == SPARSP_F32 && !a.k_scales ? 16 : 32;
     if (a.window) {  // (the most that a tile's Span is long)
         const int64_t tokens = std::min<int64_t>(most_new, r.rows / G + 2);
         const int64_t seen = int64_t(a.sinks) + a.window + tokens + 2 * r.plan.grain;
@@ -414,7 +414,7 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     // (a grid holds fewer than 2^32 threads, and units are rounded up to the eight XCDs)
     const int64_t room = std::max<int64_t>(1, (int64_t(1) << 22) / std::max<int64_t>(pairs, 8));
     tiles = std::min(tiles, room);
-    const int round = c.dtype == SPARSP_F32 ? 64 : 128;  // keys
+    const int round = c.dtype == SPARSP_F32 && !a.k_scales ? 64 : 128;  // keys
     const int64_t rounds = (int64_t(most_kv) + round - 1) / round;
     // Row tiles that can have work.
     const int64_t flat = a.tokens * int64_t(G) / r.rows + c.B;
@@ -464,6 +464,17 @@ hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
 
 hipError_t launch_few(const PagedArgs& a, const Shape& r, hipStream_t s) {
     const bool small = a.cache.d <= 64, few = r.rows == 16;
+    if (a.k_scales) {
+        if (a.cache.dtype == SPARSP_BF16)
+            return !small ? launch_rows<Four<1>, 128, 1>(a, r.plan, s)
+                   : few  ? launch_rows<Four<1>, 64, 1>(a, r.plan, s)
+                          : launch_rows<Four<1>, 64, 2>(a, r.plan, s);
+        if (few)
+            return small ? launch_rows<Four<3>, 64, 1>(a, r.plan, s)
+                         : launch_rows<Four<3>, 128, 1>(a, r.plan, s);
+        return small ? launch_rows<Four<3>, 64, 2>(a, r.plan, s)
+                     : launch_rows<Four<3>, 128, 2>(a, r.plan, s);
+    }
     if (a.cache.dtype == SPARSP_BF16)
         return !small ? launch_rows<uint16_t, 128, 1>(a, r.plan, s)
                : few  ? launch_rows<uint16_t, 64, 1>(a, r.plan, s)

@@ -23,7 +23,7 @@
 // const, i < 2, j < 4) on their own 32 bytes.
 #include <type_traits>
 
-#include "paged_plan.h"
+#include "paged_four.h"
 
 namespace sparsp {
 namespace {
@@ -88,7 +88,7 @@ __device__ __forceinline__ void copy_rows(const u32x4_t& desc, const int (&off)[
 
 // D: channels of a row in LDS; those from C on are zero and left out of the products (d = 96,
 // 32 heads, 675 tokens over 24,153: 283 us, with all 128 328 us).
-template <int D, int C, bool WINDOW>
+template <int D, int C, bool WINDOW, bool FOUR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     constexpr int TILE = kKeys * D;
@@ -122,6 +122,8 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const uint64_t head_at = uint64_t(uint32_t(hk * c.page)) * row_bytes;
     const uint64_t k_base = (reinterpret_cast<uint64_t>(c.K) & 0xffffffffffffull) + head_at;
     const uint64_t v_base = (reinterpret_cast<uint64_t>(c.V) & 0xffffffffffffull) + head_at;
+    [[maybe_unused]] FourStage<D> stage;
+    if constexpr (FOUR) stage.init(tid);
     const uint32_t k_lds = __builtin_amdgcn_readfirstlane(
         uint32_t(reinterpret_cast<uintptr_t>(&lds[0][0][16 * wave * D])));
 
@@ -250,13 +252,31 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 copy_rows<NI>(desc, voff, k_lds + (buf * 2 + 1) * TILE * 2);
             };
 
+            // 4 bits: a tile's codes are loaded two tiles ahead, and become bf16 rows one ahead.
+            auto fetch = [&](int t0) {
+                const int key = t0 + stage.key;
+                const int token = WINDOW ? span.cached(key) : key;
+                const int p = page_list[(key >> list_shift) - p0];
+                stage.load(a, token < s.kv ? p : -1, hk, token);
+            };
+            auto put = [&](auto buf_c) {
+                constexpr int buf = decltype(buf_c)::value;
+                stage.store(lds[buf][0], lds[buf][1], k_swizzle<D>(stage.key),
+                            v_swizzle<D>(stage.key));
+            };
+
             auto step = [&](int t0, auto buf_c) {
                 constexpr int buf = decltype(buf_c)::value;
                 // Each wave waits for its own copies; the barrier then publishes the tile, and
                 // everyone is done with the one before.
-                __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+                if constexpr (!FOUR) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
                 __syncthreads();
-                if (t0 + kKeys < seg_end) issue(t0 + kKeys, std::integral_constant<int, buf ^ 1>{});
+                if constexpr (FOUR) {
+                    if (t0 + kKeys < seg_end) put(std::integral_constant<int, buf ^ 1>{});
+                    if (t0 + 2 * kKeys < seg_end) fetch(t0 + 2 * kKeys);
+                } else if (t0 + kKeys < seg_end) {
+                    issue(t0 + kKeys, std::integral_constant<int, buf ^ 1>{});
+                }
                 if (t0 >= highest) return;  // no row of this wave sees any of it
                 if (WINDOW && t0 + kKeys <= earliest && t0 >= a.sinks) return;
 
@@ -403,7 +423,13 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 }
             };
 
-            issue(seg, std::integral_constant<int, 0>{});
+            if constexpr (FOUR) {
+                fetch(seg);
+                put(std::integral_constant<int, 0>{});
+                if (seg + kKeys < seg_end) fetch(seg + kKeys);
+            } else {
+                issue(seg, std::integral_constant<int, 0>{});
+            }
             for (int t0 = seg; t0 < seg_end; t0 += 2 * kKeys) {
                 step(t0, std::integral_constant<int, 0>{});
                 if (t0 + kKeys < seg_end) step(t0 + kKeys, std::integral_constant<int, 1>{});
@@ -451,16 +477,21 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     }
 }
 
+template <bool WINDOW, bool FOUR>
+auto tiles_kernel(int d) {
+    return d <= 64   ? paged_tiles_kernel<64, 64, WINDOW, FOUR>
+           : d <= 96 ? paged_tiles_kernel<128, 96, WINDOW, FOUR>
+                     : paged_tiles_kernel<128, 128, WINDOW, FOUR>;
+}
+
 }  // namespace
 
 hipError_t launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
-    const int grid = workgroups(p, a.cache), d = a.cache.d;
-    const auto kernel = a.window ? (d <= 64   ? paged_tiles_kernel<64, 64, true>
-                                    : d <= 96 ? paged_tiles_kernel<128, 96, true>
-                                              : paged_tiles_kernel<128, 128, true>)
-                                 : (d <= 64   ? paged_tiles_kernel<64, 64, false>
-                                    : d <= 96 ? paged_tiles_kernel<128, 96, false>
-                                              : paged_tiles_kernel<128, 128, false>);
+    const int grid = workgroups(p, a.cache);
+    const auto kernel = a.k_scales ? (a.window ? tiles_kernel<true, true>(a.cache.d)
+                                               : tiles_kernel<false, true>(a.cache.d))
+                                   : (a.window ? tiles_kernel<true, false>(a.cache.d)
+                                               : tiles_kernel<false, false>(a.cache.d));
     kernel<<<grid, 256, 0, s>>>(a, p);
     return hipGetLastError();
 }

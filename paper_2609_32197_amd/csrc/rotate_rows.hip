@@ -73,30 +73,14 @@ __device__ __forceinline__ void put(Vec<T, V>* p, Vec<T, V> x, bool stream) {
     *p = x;
 }
 
-// A workgroup's places: for each token the byte offset of its row in the pages, kNoPlace, or
-// kNoSequence for a column of no sequence, which nothing is written for. A wave takes a token:
-// new_off is ascending, so the token's sequence is the number of ends new_off[1..B] at or before
-// it, counted 64 at a time.
-constexpr int64_t kNoPlace = -1, kNoSequence = -2;
+// A workgroup's places: for each token the byte offset of its row in the pages, or what place_of
+// has for none. A wave takes a token.
 template <typename T>
 __device__ __forceinline__ void find_places(const Params& p, int t0, int count, int64_t* place) {
     const sparsp_cache& c = p.cache;
     const int lane = threadIdx.x & 63;
     for (int k = threadIdx.x >> 6; k < count; k += kThreads / 64) {
-        int b = 0;
-        for (int e = lane; e < c.B; e += 64) b += c.new_off[e + 1] <= t0 + k;
-        for (int off = 32; off; off >>= 1) b += __shfl_xor(b, off);
-        int64_t row = kNoSequence;  // of head 0
-        if (b < c.B) {
-            const Seq s = sequence(c, p.tokens, b);
-            const int i = t0 + k - s.q0, slot = s.kv - s.n + i;
-            if (i >= 0 && i < s.n) row = kNoPlace;
-            if (row == kNoPlace && slot >= 0) {
-                const int shift = __builtin_ctz(c.page);
-                const int page = page_of(c.table, c.width, c.pages, b, slot >> shift);
-                if (page >= 0) row = int64_t(page) * c.H * c.page + (slot & (c.page - 1));
-            }
-        }
+        const int64_t row = place_of(c, p.tokens, t0 + k, lane);
         if (lane == 0) place[k] = row < 0 ? row : row * c.d * int64_t(sizeof(T));
         if (row >= 0 && c.weights)
             for (int h = lane; h < c.H; h += 64) c.weights[row + int64_t(h) * c.page] = 0.f;

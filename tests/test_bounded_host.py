@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2609_32197_amd as sp
+from paper_2609_32197_amd.bounded import _CACHE4
 from paper_2609_32197_amd.paged import _CACHE, _ROWS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -85,3 +86,118 @@ def test_binding_refuses_a_window_without_a_gpu():
     off, kv = torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError, match="GPU"):
         sp.sparsp_paged_attn(x, c, c, i, off, kv, window=5)
+
+
+# ---------------------------------------------------------------------------
+# the 4-bit cache
+# ---------------------------------------------------------------------------
+
+
+def cache4(**kw):
+    v = dict(K=AT, Ks=2 * AT, V=3 * AT, Vs=4 * AT, table=AT, new_off=AT, kv_len=AT, pages=9, H=2,
+             page=16, d=64, width=4, B=3, r0=0, r1=0)
+    v.update(kw)
+    return _CACHE4.pack(*v.values())
+
+
+ROTARY = sp.Rotary(64)._pack(False)
+
+
+def append4(c=None, dtype=sp.BF16, K=None, V=None, r=ROTARY, pos=AT, bits=32, Q=None, Qo=None, tokens=5):
+    return sp.load_library().sparsp_paged_append4(
+        c or cache4(), tokens, dtype, K or rows(heads=2), V or rows(6 * AT, heads=2), r, pos, bits, AT,
+        Q, Qo, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(c=cache4(d=48)), "SPARSP_E_UNSUPPORTED", "multiple of 32"),
+    (dict(c=cache4(d=160)), "SPARSP_E_UNSUPPORTED", "multiple of 32"),
+    (dict(c=cache4(d=0)), "SPARSP_E_INVALID", "d = 0"),
+    (dict(c=cache4(page=8)), "SPARSP_E_UNSUPPORTED", "page"),
+    (dict(c=cache4(Ks=0)), "SPARSP_E_INVALID", "NULL"),
+    (dict(c=cache4(Vs=AT + 8)), "SPARSP_E_INVALID", "aligned"),
+    (dict(c=cache4(V=AT)), "SPARSP_E_INVALID", "same memory"),
+    (dict(c=cache4(Vs=2 * AT)), "SPARSP_E_INVALID", "same memory"),
+    (dict(dtype=5), "SPARSP_E_DTYPE", "dtype"),
+    (dict(K=rows(heads=3)), "SPARSP_E_INVALID", "heads"),
+    (dict(K=rows(3 * AT + 2, heads=2)), "SPARSP_E_INVALID", "16 bytes"),
+    (dict(bits=16), "SPARSP_E_DTYPE", "position_bits"),
+    (dict(pos=0), "SPARSP_E_INVALID", "positions"),
+    (dict(Q=rows(7 * AT)), "SPARSP_E_INVALID", "Q_out"),
+    (dict(Q=rows(7 * AT), Qo=rows(8 * AT), r=None), "SPARSP_E_INVALID", "rotation"),
+    (dict(Q=rows(7 * AT), Qo=rows(3 * AT)), "SPARSP_E_INVALID", "Q_out"),
+    (dict(Q=rows(7 * AT), Qo=rows(8 * AT, heads=5)), "SPARSP_E_INVALID", "heads"),
+    (dict(Q=rows(7 * AT), Qo=_ROWS.pack(8 * AT, 64, 64, 4, 0)), "SPARSP_E_INVALID", "overlap"),
+    (dict(tokens=-1), "SPARSP_E_INVALID", "tokens"),
+])
+def test_append4_refused(kw, code, word):
+    got, message = status(append4(**kw))
+    assert got == code and word in message
+
+
+@pytest.mark.parametrize("K,V,word", [
+    (rows(heads=2), rows(heads=2), "same memory"),
+    (rows(heads=1), rows(6 * AT, heads=2), "heads"),
+    (rows(heads=2), _ROWS.pack(6 * AT, 64, 64, 2, 0), "overlap"),
+])
+def test_read4_refused(K, V, word):
+    _, message = status(sp.load_library().sparsp_paged_read4(cache4(), 5, sp.F32, K, V, None))
+    assert word in message
+
+
+def attn4(c=None, dtype=sp.BF16, O=None, out=sp.BF16, causal=1, window=0, sinks=0, nbytes=0):
+    return sp.load_library().sparsp_paged_attn4(
+        c or cache4(), 5, dtype, rows(), O or rows(5 * AT), out, None, causal, window, sinks, 0.1, 0, 0,
+        None, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(window=-1), "SPARSP_E_INVALID", "window"),
+    (dict(window=4, sinks=-1), "SPARSP_E_INVALID", "sinks"),
+    (dict(sinks=4), "SPARSP_E_INVALID", "sinks need a window"),
+    (dict(window=4, causal=0), "SPARSP_E_INVALID", "causal"),
+    (dict(dtype=sp.F32), "SPARSP_E_DTYPE", "f32"),
+    (dict(c=cache4(H=3)), "SPARSP_E_INVALID", "query heads"),
+    (dict(c=cache4(V=0)), "SPARSP_E_INVALID", "NULL"),
+    (dict(O=rows()), "SPARSP_E_INVALID", "O may not be Q"),
+    (dict(nbytes=-1), "SPARSP_E_INVALID", "workspace_bytes"),
+])
+def test_attn4_refused(kw, code, word):
+    got, message = status(attn4(**kw))
+    assert got == code and word in message
+
+
+def test_nothing_to_do():
+    one = rows(heads=2, tokens=1), rows(6 * AT, heads=2, tokens=1)
+    assert append4(tokens=0, K=one[0], V=one[1]) == 0
+    assert sp.load_library().sparsp_paged_read4(cache4(), 0, sp.F32, *one, None) == 0
+
+
+def test_attn4_workspace():
+    c = sp.Cache4.zeros(4, 2, 16, 64, device="cpu")
+    t = torch.zeros(2, 3000, dtype=torch.int32)
+    whole = sp.sparsp_paged_attn4_workspace_bytes(c, t, 2, 4, 1)
+    some = sp.sparsp_paged_attn4_workspace_bytes(c, t, 2, 4, 1, window=4000)
+    assert 0 < some < whole
+    assert sp.sparsp_paged_attn4_workspace_bytes(c, t, 2, 4, 1, 100, dtype=torch.float32) == 0
+    with pytest.raises(sp.SparspError):
+        sp.sparsp_paged_attn4_workspace_bytes(c, t, 2, 3)
+    for kw in (dict(window=0), dict(sinks=1), dict(dtype=torch.float16)):
+        with pytest.raises(ValueError):
+            sp.sparsp_paged_attn4_workspace_bytes(c, t, 2, 4, **kw)
+
+
+def test_binding_of_the_4_bit_cache_wants_the_gpu():
+    c = sp.Cache4.zeros(4, 2, 16, 64, device="cpu")
+    x = torch.zeros(2, 3, 64, dtype=torch.bfloat16)
+    i = torch.zeros(1, 4, dtype=torch.int32)
+    off, kv = torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    for call in (lambda: sp.sparsp_paged_append4(x, x, c, i, off, kv),
+                 lambda: sp.sparsp_paged_read4(c, i, off, kv, 3),
+                 lambda: sp.sparsp_paged_attn4(x, c, i, off, kv)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    with pytest.raises(TypeError):
+        sp.sparsp_paged_attn4(x, c.K, i, off, kv)
+    with pytest.raises(ValueError):
+        sp.Cache4.zeros(4, 2, 16, 48, device="cpu")
