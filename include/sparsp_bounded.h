@@ -1,11 +1,17 @@
 /*
  * sparsp_bounded.h - C ABI of libsparsp for a paged cache (sparsp_cache.h) that is kept bounded: a
- * sliding window bounds what a token reads of it, and 4 bits a value what it weighs.
+ * sliding window bounds what a token reads of it, 4 bits a value what it weighs, and pages are
+ * shared, given back and moved together.
  *
  *   sparsp_paged_attn_window  attention over the latest tokens and a few first ones
  *   sparsp_paged_append4      new tokens' K and V into a cache of 4-bit values, K (and Q) rotated
  *   sparsp_paged_attn4        attention over such a cache, with or without a window
  *   sparsp_paged_read4        what such a cache holds of its latest tokens, back as rows
+ *   sparsp_pages_reserve      pages for the tokens that come next
+ *   sparsp_pages_release      back what no later token sees
+ *   sparsp_pages_fork         sequences continue others, ended ones go
+ *   sparsp_pages_compact      the pages in use moved together
+ *   sparsp_pages_copy         contents of pages to others
  *
  * The conventions of sparsp.h and sparsp_cache.h hold.
  */
@@ -94,6 +100,90 @@ int64_t sparsp_paged_attn4_workspace_bytes(const sparsp_cache4* cache, int32_t t
  */
 int sparsp_paged_read4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype,
                        const sparsp_rows* K, const sparsp_rows* V, void* stream);
+
+/*
+ * The pages of a cache and the sequences that use them. refs[p] counts the table entries that name
+ * page p, and whatever else the caller counts as holding it (a prefix that is kept, say): 0 or less
+ * is a free page. Tables that several calls share (one for each cache of a layer, or one for all) name
+ * pages of the same numbers. Entries outside [0, pages) name no page. pages <= 2^30, B <= 65536,
+ * B * width <= 2^30, width * page <= 2^30, page as in sparsp_cache.
+ *
+ * Calls work on the counts and tables as they find them on the stream: nothing comes back to the
+ * host, so a step can be captured. Pages are taken lowest number first, in the order of the
+ * entries that want them (by row, then by place), so results depend on the arguments only. Where a
+ * call runs out of free pages the last of these entries name none, and *left, which otherwise is the
+ * number of pages still free, is minus the number that is missing. Whatever these arrays hold, no
+ * kernel leaves them, or the buffers.
+ */
+typedef struct {
+    int32_t* refs;         /* [pages] */
+    int32_t* table;        /* [B, width] */
+    const int32_t* kv_len; /* [B] */
+    int32_t pages, page, width, B;
+} sparsp_pages;
+
+/* [pages, page_bytes] of device memory: K, V, weights, codes or scales of a cache. 16-byte aligned,
+ * page_bytes a multiple of 16 up to 2^32; at most 8 in a call, no memory twice. */
+typedef struct {
+    void* data;
+    int64_t page_bytes;
+} sparsp_page_buffer;
+
+/* Workspace bytes of the calls below for these pages and rows (of a fork; otherwise B), or a negative
+ * status. Host only; the pointers are not read. A workspace is 16-byte aligned device memory,
+ * contents irrelevant, not shared by calls that overlap; one that is too small is SPARSP_E_CAPACITY. */
+int64_t sparsp_pages_workspace_bytes(const sparsp_pages* pages, int32_t rows);
+
+/*
+ * Pages for the new tokens kv_len - n .. kv_len - 1 of every sequence (n = new_off[b+1] - new_off[b],
+ * as for the append that follows): entries among theirs that name no page get a free one, its count
+ * 1. The page that a sequence's last old token is on must be its own, as sparsp_pages_fork sees to.
+ */
+int sparsp_pages_reserve(const sparsp_pages* pages, const int32_t* new_off, int32_t* left,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Entries that no later token needs come to name no page, and their pages' counts go down by one:
+ * those behind kv_len tokens (kv_len = 0 ends a sequence, a smaller kv_len takes tokens back), and
+ * with window > 0 those all of whose tokens t lie in sinks <= t <= kv_len - window, which the next
+ * token of a sequence of kv_len does not see (sparsp_paged_attn_window). window 0: none.
+ */
+int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sinks, void* stream);
+
+/*
+ * Row i of the new tables continues the old row parents[i] (outside [0, B): an empty sequence), for
+ * any number of rows; old rows that none continues end. Full pages are shared. A page that is filled
+ * in part stays with the first row that continues its sequence if its count was 1, and is copied for
+ * every other, in all the buffers, to a page of its own (never one that the call copies from). Counts: refs_out is refs less the old
+ * table's entries and with the new one's. The old table, counts and lengths stay as they are; contents
+ * of pages that it names stay as long as nothing is written to the new one's.
+ *
+ * table_out [rows, width], kv_len_out [rows], refs_out [pages], left [1].
+ */
+int sparsp_pages_fork(const sparsp_pages* pages, const int32_t* parents, int32_t rows,
+                      const sparsp_page_buffer* buffers, int32_t count, int32_t* table_out,
+                      int32_t* kv_len_out, int32_t* refs_out, int32_t* left, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/*
+ * With n pages in use, those numbered n and above move, contents and counts, to the free ones below
+ * n, lowest to lowest; *live is n. The pages from n on are free then, and may be given up. table_out
+ * [B, width] and refs_out [pages] are the new ones; entries that name no page, or a free one, become
+ * -1. The old table, and the contents that it names, stay as they are. kv_len and page are not used
+ * (page must be valid). Only the rows of this table are rewritten: other holders of a page follow it
+ * by themselves.
+ */
+int sparsp_pages_compact(const sparsp_pages* pages, const sparsp_page_buffer* buffers, int32_t count,
+                         int32_t* table_out, int32_t* refs_out, int32_t* live, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/*
+ * Page src[k] of every buffer to page dst[k], k < moves (device int32 arrays); a number outside [0,
+ * pages) copies nothing. No page may be both a source and a destination, or a destination twice (it
+ * would hold any of the contents).
+ */
+int sparsp_pages_copy(const sparsp_page_buffer* buffers, int32_t count, int32_t pages,
+                      const int32_t* src, const int32_t* dst, int32_t moves, void* stream);
 
 #ifdef __cplusplus
 }

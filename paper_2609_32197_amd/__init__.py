@@ -46,6 +46,11 @@ The cache kept bounded (bounded.py, include/sparsp_bounded.h):
     sparsp_paged_append4           new tokens into a cache of 4-bit values
     sparsp_paged_attn4             attention over such a cache
     sparsp_paged_read4             what such a cache holds, back as rows
+    sparsp_pages_reserve           pages for the tokens that come next
+    sparsp_pages_release           back what no later token sees
+    sparsp_pages_fork              sequences continue others, ended ones go
+    sparsp_pages_compact           the pages in use moved together
+    sparsp_pages_copy              contents of pages to others
 
 Calls run on the current stream, or on `stream` where one is given. Outputs that a call makes itself
 come from the memory of that stream: wait for it before they are used on another.

@@ -4,6 +4,11 @@
     sparsp_paged_append4      new tokens' K and V into it, K and Q rotated on the way
     sparsp_paged_attn4        attention of the new tokens over it, with or without a window
     sparsp_paged_read4        what it holds of the new tokens, back as rows
+    sparsp_pages_reserve      pages for the tokens that come next
+    sparsp_pages_release      back what no later token sees
+    sparsp_pages_fork         sequences continue others, ended ones go
+    sparsp_pages_compact      the pages in use moved together
+    sparsp_pages_copy         contents of pages to others
 
 Attention with a window over a cache of rows is sparsp_paged_attn(window=, sinks=). Token tensors, page
 tables, lengths, devices and streams are as for the paged cache (paged.py).
@@ -30,6 +35,18 @@ __all__ = [
     "paged_attn4",
     "paged_attn4_workspace_bytes",
     "paged_read4",
+    "sparsp_pages_reserve",
+    "sparsp_pages_release",
+    "sparsp_pages_fork",
+    "sparsp_pages_compact",
+    "sparsp_pages_copy",
+    "sparsp_pages_workspace_bytes",
+    "pages_reserve",
+    "pages_release",
+    "pages_fork",
+    "pages_compact",
+    "pages_copy",
+    "pages_workspace_bytes",
 ]
 
 _VP, _I32, _I64, _F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -43,8 +60,17 @@ _SIGNATURES.update({
                            _I32, _I32, _VP, _I64, _VP],
     "sparsp_paged_attn4_workspace_bytes": [_STRUCT, _I32, _I32, _I32, _I32, _I32, _I32, _I32],
     "sparsp_paged_read4": [_STRUCT, _I32, _I32, _STRUCT, _STRUCT, _VP],
+    "sparsp_pages_workspace_bytes": [_STRUCT, _I32],
+    "sparsp_pages_reserve": [_STRUCT, _VP, _VP, _VP, _I64, _VP],
+    "sparsp_pages_release": [_STRUCT, _I32, _I32, _VP],
+    "sparsp_pages_fork": [_STRUCT, _VP, _I32, _STRUCT, _I32, _VP, _VP, _VP, _VP, _VP, _I64, _VP],
+    "sparsp_pages_compact": [_STRUCT, _STRUCT, _I32, _VP, _VP, _VP, _VP, _I64, _VP],
+    "sparsp_pages_copy": [_STRUCT, _I32, _I32, _VP, _VP, _I32, _VP],
 })
 _RESTYPES["sparsp_paged_attn4_workspace_bytes"] = _I64
+_RESTYPES["sparsp_pages_workspace_bytes"] = _I64
+_PAGES = struct.Struct("@PPPiiii")
+_BUFFER = struct.Struct("@Pq")
 
 
 @dataclass(frozen=True)
@@ -211,7 +237,164 @@ def sparsp_paged_attn4(Q, cache: Cache4, page_table, new_off, kv_len, causal: bo
     return o, ls
 
 
+# ---------------------------------------------------------------------------
+# pages
+# ---------------------------------------------------------------------------
+
+
+def _pages(refs, page_table, kv_len, page):
+    """(sparsp_pages, GPU, its shape)."""
+    torch = _torch()
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be an int32 [B, width] tensor")
+    at = _on(refs, "refs", None, torch.int32)
+    if refs.dim() != 1:
+        raise ValueError("refs must be an int32 [pages] tensor")
+    dev, (B, width) = refs.get_device(), page_table.shape
+    return _PAGES.pack(at, _on(page_table, "page_table", dev, torch.int32),
+                       0 if kv_len is None else _on(kv_len, "kv_len", dev, torch.int32, (B,)),
+                       refs.shape[0], _int(page, "page"), width, B), dev
+
+
+def _buffers(caches, pages, dev):
+    """(sparsp_page_buffers, how many) of tensors [pages, ...] and Cache4s."""
+    torch = _torch()
+    if isinstance(caches, (torch.Tensor, Cache4)):
+        caches = (caches,)
+    packed, count = b"", 0
+    for c in caches:
+        for t in c.tensors if isinstance(c, Cache4) else (c,):
+            at = _on(t, "a cache", dev)
+            if t.dim() < 2 or t.shape[0] != pages:
+                raise ValueError(f"a cache must be [pages = {pages}, ...] (got {tuple(t.shape)})")
+            packed += _BUFFER.pack(at, t.numel() // pages * t.element_size())
+            count += 1
+    return packed or None, count
+
+
+def _page_workspace(packed, rows, workspace, like, dev, stream):
+    """Address and bytes of a page call's workspace, and the tensor that holds it."""
+    if workspace is None:
+        nbytes = int(load_library().sparsp_pages_workspace_bytes(packed, rows))
+        _check(nbytes if nbytes < 0 else 0)
+        workspace = _new(like, (nbytes,), _torch().uint8, stream)
+    return _on(workspace, "workspace", dev), workspace.numel() * workspace.element_size(), workspace
+
+
+def _out(t, name, like, shape, dev, stream):
+    """(int32 tensor, address), made here unless given."""
+    i32 = _torch().int32
+    if t is None:
+        t = _new(like, shape, i32, stream)
+    return t, _on(t, name, dev, i32, shape)
+
+
+def sparsp_pages_workspace_bytes(refs, page_table, rows: int = 0) -> int:
+    """Workspace bytes of the page calls for these shapes and a fork's rows (host)."""
+    B, width = page_table.shape
+    n = int(load_library().sparsp_pages_workspace_bytes(
+        _PAGES.pack(0, 0, 0, refs.shape[0], 16, width, B), _int(rows, "rows")))
+    _check(n if n < 0 else 0)
+    return n
+
+
+def sparsp_pages_reserve(refs, page_table, new_off, kv_len, page: int, left=None, workspace=None,
+                         stream=None):
+    """Pages for the new tokens of every sequence, where page_table names none: before their append.
+
+    refs int32 [pages] counts the entries that name a page; it and page_table are changed in place.
+    kv_len counts the new tokens. Returns left, int32 [1]: the free pages left, or minus the number
+    that was missing. A workspace is allocated here unless one is given, like left.
+    """
+    p, dev = _pages(refs, page_table, kv_len, page)
+    B = page_table.shape[0]
+    left, at = _out(left, "left", refs, (1,), dev, stream)
+    ws, nbytes, workspace = _page_workspace(p, B, workspace, refs, dev, stream)
+    _call(load_library().sparsp_pages_reserve, dev, stream, p,
+          _on(new_off, "new_off", dev, _torch().int32, (B + 1,)), at, ws, nbytes)
+    return left
+
+
+def sparsp_pages_release(refs, page_table, kv_len, page: int, window: Optional[int] = None,
+                         sinks: int = 0, stream=None):
+    """Gives back, in place, the pages that no later token of the sequences sees.
+
+    Those behind kv_len tokens (0 ends a sequence), and with a window those between the first `sinks`
+    tokens and the window of the next one. Their entries become -1. Returns refs.
+    """
+    p, dev = _pages(refs, page_table, kv_len, page)
+    _call(load_library().sparsp_pages_release, dev, stream, p, *_checked(window, sinks, True))
+    return refs
+
+
+def sparsp_pages_fork(refs, page_table, kv_len, parents, page: int, caches=(), page_table_out=None,
+                      kv_len_out=None, refs_out=None, left=None, workspace=None, stream=None):
+    """Row i of the new tables continues row parents[i] of the old ones (-1: an empty sequence).
+
+    Full pages are shared, partly filled ones copied in all `caches` (tensors [pages, ...] or Cache4s)
+    for all but the first row that continues a sequence; sequences that none continues end. Returns
+    (page_table, kv_len, refs, left); the old tensors stay as they are.
+    """
+    torch = _torch()
+    p, dev = _pages(refs, page_table, kv_len, page)
+    at = _on(parents, "parents", dev, torch.int32)
+    if parents.dim() != 1:
+        raise ValueError("parents must be an int32 [rows] tensor")
+    rows, pages, width = parents.shape[0], refs.shape[0], page_table.shape[1]
+    buffers, count = _buffers(caches, pages, dev)
+    table, t = _out(page_table_out, "page_table_out", refs, (rows, width), dev, stream)
+    kv, k = _out(kv_len_out, "kv_len_out", refs, (rows,), dev, stream)
+    counts, r = _out(refs_out, "refs_out", refs, (pages,), dev, stream)
+    left, l = _out(left, "left", refs, (1,), dev, stream)
+    ws, nbytes, workspace = _page_workspace(p, rows, workspace, refs, dev, stream)
+    _call(load_library().sparsp_pages_fork, dev, stream, p, at, rows, buffers, count, t, k, r, l, ws,
+          nbytes)
+    return table, kv, counts, left
+
+
+def sparsp_pages_compact(refs, page_table, caches=(), page_table_out=None, refs_out=None, live=None,
+                         workspace=None, stream=None):
+    """Moves the pages in use together: of n, those numbered n and above into the free ones below.
+
+    Contents move in all `caches` (tensors [pages, ...] or Cache4s). Returns (page_table, refs, live)
+    with live int32 [1] = n; the old tensors stay as they are, and the old pages' contents too.
+    """
+    p, dev = _pages(refs, page_table, None, 16)
+    (B, width), pages = page_table.shape, refs.shape[0]
+    buffers, count = _buffers(caches, pages, dev)
+    table, t = _out(page_table_out, "page_table_out", refs, (B, width), dev, stream)
+    counts, r = _out(refs_out, "refs_out", refs, (pages,), dev, stream)
+    live, l = _out(live, "live", refs, (1,), dev, stream)
+    ws, nbytes, workspace = _page_workspace(p, B, workspace, refs, dev, stream)
+    _call(load_library().sparsp_pages_compact, dev, stream, p, buffers, count, t, r, l, ws, nbytes)
+    return table, counts, live
+
+
+def sparsp_pages_copy(src, dst, caches, stream=None):
+    """Page src[k] of every cache (tensors [pages, ...] or Cache4s) to page dst[k]; int32 tensors.
+
+    Numbers of no page copy nothing. No page may be a source and a destination, nor a destination twice.
+    """
+    torch = _torch()
+    s = _on(src, "src", None, torch.int32)
+    dev, n = src.get_device(), src.numel()
+    caches = (caches,) if isinstance(caches, (torch.Tensor, Cache4)) else tuple(caches)
+    if not caches:
+        raise ValueError("nothing to copy")
+    first = caches[0]
+    pages = (first.K if isinstance(first, Cache4) else first).shape[0]
+    buffers, count = _buffers(caches, pages, dev)
+    _call(load_library().sparsp_pages_copy, dev, stream, buffers, count, pages, s,
+          _on(dst, "dst", dev, torch.int32, src.shape), n)
+
+
 paged_append4 = sparsp_paged_append4
 paged_attn4 = sparsp_paged_attn4
 paged_attn4_workspace_bytes = sparsp_paged_attn4_workspace_bytes
 paged_read4 = sparsp_paged_read4
+pages_reserve = sparsp_pages_reserve
+pages_release = sparsp_pages_release
+pages_fork = sparsp_pages_fork
+pages_compact = sparsp_pages_compact
+pages_copy = sparsp_pages_copy
+pages_workspace_bytes = sparsp_pages_workspace_bytes

@@ -73,6 +73,84 @@ int check_attn4(const sparsp_cache4* cache, int tokens, int dtype, const sparsp_
     return SPARSP_OK;
 }
 
+int check_pages(const sparsp_pages* p, bool lengths) {
+    if (!p) return fail(SPARSP_E_INVALID, "pages is NULL");
+    if (!p->refs || !p->table || (lengths && !p->kv_len))
+        return fail(SPARSP_E_INVALID, "NULL pointer of pages");
+    if (p->pages < 1 || p->width < 1 || p->B < 1)
+        return fail(SPARSP_E_INVALID, "pages, width and B must be positive (%d, %d, %d)", p->pages,
+                    p->width, p->B);
+    if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1)))
+        return fail(SPARSP_E_UNSUPPORTED, "page = %d must be a power of two from 16 to 256", p->page);
+    if (p->pages > (1 << 30) || p->B > 65536 || int64_t(p->B) * p->width > (int64_t(1) << 30) ||
+        int64_t(p->width) * p->page > (int64_t(1) << 30))
+        return fail(SPARSP_E_UNSUPPORTED, "pages, B * width or width * page exceed 2^30, or B 65536");
+    return SPARSP_OK;
+}
+
+int check_buffers(const sparsp_page_buffer* b, int count, sparsp::PageBuffers* f) {
+    if (count < 0 || count > sparsp::kMaxBuffers || (count > 0 && !b))
+        return fail(SPARSP_E_INVALID, "%d buffers, 0 to %d are supported", count, sparsp::kMaxBuffers);
+    *f = {};
+    int64_t units = 0;
+    for (int i = 0; i < count; ++i) {
+        if (!b[i].data || !aligned16(b[i].data))
+            return fail(SPARSP_E_INVALID, "buffer %d must be 16-byte aligned memory", i);
+        if (b[i].page_bytes < 16 || b[i].page_bytes % 16 || b[i].page_bytes > (int64_t(1) << 32))
+            return fail(SPARSP_E_INVALID, "buffer %d: a page of %lld bytes is no multiple of 16", i,
+                        (long long)b[i].page_bytes);
+        for (int j = 0; j < i; ++j)
+            if (b[j].data == b[i].data)
+                return fail(SPARSP_E_INVALID, "buffers %d and %d are the same memory", j, i);
+        f->data[i] = static_cast<char*>(b[i].data);
+        f->bytes[i] = b[i].page_bytes;
+        f->first[i] = int(units);
+        units += (b[i].page_bytes + sparsp::kPageUnit - 1) / sparsp::kPageUnit;
+    }
+    f->count = count;
+    f->units = int(units);
+    return SPARSP_OK;
+}
+
+// The workspace: what a call counts and lists. Returns its size in bytes.
+constexpr int kScanPages = 16384, kScanRows = 1024;  // at most so many a count
+int64_t lay_out(const sparsp_pages* p, int rows, void* workspace, sparsp::PageArgs* a) {
+    const int64_t counts = ((p->pages + kScanPages - 1) / kScanPages + (rows + kScanRows - 1) / kScanRows + 3) / 4 * 4;
+    int32_t* at = static_cast<int32_t*>(workspace);
+    const int64_t total = 4 * (4 + counts + int64_t(3) * p->pages + rows);
+    if (!at) return total;
+    a->moves = at;
+    a->counts = at + 4;
+    a->src = a->counts + counts;
+    a->dst = a->src + p->pages;
+    a->to = a->dst + p->pages;
+    a->from = a->to + p->pages;
+    return total;
+}
+
+int check_workspace(const sparsp_pages* p, int rows, void* workspace, int64_t bytes,
+                    sparsp::PageArgs* a) {
+    if (!workspace || !aligned16(workspace))
+        return fail(SPARSP_E_INVALID, "workspace must be 16-byte aligned memory");
+    const int64_t need = lay_out(p, rows, workspace, a);
+    if (bytes < need)
+        return fail(SPARSP_E_CAPACITY, "workspace of %lld bytes, %lld are needed", (long long)bytes,
+                    (long long)need);
+    return SPARSP_OK;
+}
+
+sparsp::PageArgs page_args(const sparsp_pages* p) {
+    sparsp::PageArgs a = {};
+    a.refs = p->refs;
+    a.table = p->table;
+    a.kv_len = p->kv_len;
+    a.pages = p->pages;
+    a.page = p->page;
+    a.width = p->width;
+    a.rows = a.old_rows = p->B;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -149,6 +227,102 @@ int sparsp_paged_attn4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype
     a.causal = causal != 0;
     a.lse = lse;
     return hip_status(sparsp::launch_paged_attn(a, (hipStream_t)stream), "sparsp_paged_attn4");
+}
+
+int64_t sparsp_pages_workspace_bytes(const sparsp_pages* pages, int32_t rows) {
+    sparsp_pages p;
+    if (!pages) return fail(SPARSP_E_INVALID, "pages is NULL");
+    p = *pages;
+    int32_t spot = 0;
+    p.refs = p.table = &spot;  // (not read)
+    if (int rc = check_pages(&p, false)) return rc;
+    if (rows < 0 || rows > 65536)
+        return fail(SPARSP_E_UNSUPPORTED, "rows = %d outside [0, 65536]", rows);
+    ok();
+    return lay_out(&p, rows > p.B ? rows : p.B, nullptr, nullptr);
+}
+
+int sparsp_pages_reserve(const sparsp_pages* pages, const int32_t* new_off, int32_t* left,
+                         void* workspace, int64_t workspace_bytes, void* stream) {
+    if (int rc = check_pages(pages, true)) return rc;
+    if (!new_off || !left) return fail(SPARSP_E_INVALID, "new_off or left is NULL");
+    sparsp::PageArgs a = page_args(pages);
+    if (int rc = check_workspace(pages, pages->B, workspace, workspace_bytes, &a)) return rc;
+    a.moves = nullptr;
+    a.from = nullptr;
+    a.new_off = new_off;
+    a.left = left;
+    return hip_status(sparsp::launch_pages_reserve(a, (hipStream_t)stream), "sparsp_pages_reserve");
+}
+
+int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sinks, void* stream) {
+    if (int rc = check_pages(pages, true)) return rc;
+    if (window < 0 || sinks < 0 || (sinks > 0 && window == 0))
+        return fail(SPARSP_E_INVALID, "window = %d and sinks = %d must not be negative, sinks need a window",
+                    window, sinks);
+    sparsp::PageArgs a = page_args(pages);
+    a.window = window < kFarthest ? window : kFarthest;
+    a.sinks = sinks;
+    return hip_status(sparsp::launch_pages_release(a, (hipStream_t)stream), "sparsp_pages_release");
+}
+
+int sparsp_pages_fork(const sparsp_pages* pages, const int32_t* parents, int32_t rows,
+                      const sparsp_page_buffer* buffers, int32_t count, int32_t* table_out,
+                      int32_t* kv_len_out, int32_t* refs_out, int32_t* left, void* workspace,
+                      int64_t workspace_bytes, void* stream) {
+    sparsp::PageBuffers f;
+    if (int rc = check_pages(pages, true)) return rc;
+    if (rows < 1 || rows > 65536 || int64_t(rows) * pages->width > (int64_t(1) << 30))
+        return fail(SPARSP_E_UNSUPPORTED, "rows = %d outside [1, 65536], or rows * width exceeds 2^30",
+                    rows);
+    if (int rc = check_buffers(buffers, count, &f)) return rc;
+    if (!parents || !table_out || !kv_len_out || !refs_out || !left)
+        return fail(SPARSP_E_INVALID, "NULL pointer of a fork");
+    if (table_out == pages->table || refs_out == pages->refs || kv_len_out == pages->kv_len)
+        return fail(SPARSP_E_INVALID, "a fork's outputs may not be its inputs");
+    sparsp::PageArgs a = page_args(pages);
+    if (int rc = check_workspace(pages, rows, workspace, workspace_bytes, &a)) return rc;
+    a.old_refs = pages->refs;
+    a.old_table = pages->table;
+    a.refs = refs_out;
+    a.table = table_out;
+    a.kv_out = kv_len_out;
+    a.parents = parents;
+    a.rows = rows;
+    a.left = left;
+    return hip_status(sparsp::launch_pages_fork(a, f, (hipStream_t)stream), "sparsp_pages_fork");
+}
+
+int sparsp_pages_compact(const sparsp_pages* pages, const sparsp_page_buffer* buffers, int32_t count,
+                         int32_t* table_out, int32_t* refs_out, int32_t* live, void* workspace,
+                         int64_t workspace_bytes, void* stream) {
+    sparsp::PageBuffers f;
+    if (int rc = check_pages(pages, false)) return rc;
+    if (int rc = check_buffers(buffers, count, &f)) return rc;
+    if (!table_out || !refs_out || !live) return fail(SPARSP_E_INVALID, "NULL pointer of a compaction");
+    if (table_out == pages->table || refs_out == pages->refs)
+        return fail(SPARSP_E_INVALID, "a compaction's outputs may not be its inputs");
+    sparsp::PageArgs a = page_args(pages);
+    if (int rc = check_workspace(pages, pages->B, workspace, workspace_bytes, &a)) return rc;
+    a.old_refs = pages->refs;
+    a.old_table = pages->table;
+    a.refs = refs_out;
+    a.table = table_out;
+    a.left = live;
+    return hip_status(sparsp::launch_pages_compact(a, f, (hipStream_t)stream), "sparsp_pages_compact");
+}
+
+int sparsp_pages_copy(const sparsp_page_buffer* buffers, int32_t count, int32_t pages,
+                      const int32_t* src, const int32_t* dst, int32_t moves, void* stream) {
+    sparsp::PageBuffers f;
+    if (pages < 1 || pages > (1 << 30)) return fail(SPARSP_E_INVALID, "pages = %d out of range", pages);
+    if (count < 1) return fail(SPARSP_E_INVALID, "nothing to copy");
+    if (int rc = check_buffers(buffers, count, &f)) return rc;
+    if (moves < 0 || moves > (1 << 30)) return fail(SPARSP_E_INVALID, "moves = %d out of range", moves);
+    if (moves == 0) return ok();
+    if (!src || !dst) return fail(SPARSP_E_INVALID, "src or dst is NULL");
+    return hip_status(sparsp::launch_pages_copy(f, src, dst, moves, pages, (hipStream_t)stream),
+                      "sparsp_pages_copy");
 }
 
 }  // extern "C"

@@ -82,4 +82,33 @@ hipError_t launch_cache_evict(const sparsp_cache& c, int keep, int first, int re
 // Bytes of workspace that its choice can use.
 int64_t evict_workspace(const sparsp_cache& c);
 
+// Pages of a cache: the tables and counts of a call, and the contents that it copies.
+struct PageArgs {
+    int32_t *refs, *table;          // written (the new ones, where there are old ones)
+    const int32_t *old_refs, *old_table;
+    const int32_t *kv_len, *new_off, *parents;
+    int32_t* kv_out;
+    int pages, page, width, rows, old_rows;
+    int window, sinks;
+    int32_t* left;    // [1]
+    // workspace
+    int32_t* moves;   // [1]
+    int32_t* counts;  // of chunks
+    int32_t *src, *dst, *to, *from;
+};
+constexpr int kMaxBuffers = 8;
+struct PageBuffers {
+    char* data[kMaxBuffers];
+    int64_t bytes[kMaxBuffers];  // of a page
+    int first[kMaxBuffers];      // of a page's copying units, each buffer's first
+    int count, units;
+};
+constexpr int kPageUnit = 16384;  // bytes of a unit at most
+hipError_t launch_pages_reserve(const PageArgs& a, hipStream_t s);
+hipError_t launch_pages_release(const PageArgs& a, hipStream_t s);
+hipError_t launch_pages_fork(const PageArgs& a, const PageBuffers& f, hipStream_t s);
+hipError_t launch_pages_copy(const PageBuffers& f, const int32_t* src, const int32_t* dst, int count,
+                             int pages, hipStream_t s);
+hipError_t launch_pages_compact(const PageArgs& a, const PageBuffers& f, hipStream_t s);
+
 }  // namespace sparsp

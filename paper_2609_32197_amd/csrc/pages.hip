@@ -1,0 +1,453 @@
+// Pages of a cache shared, taken, given back, copied and moved together.
+//
+// refs[p] counts the table entries (and other holders) of page p; a page with none (or fewer) is
+// free. Whatever takes pages takes the lowest free ones, in the order of the entries that want them,
+// so that results depend on the arguments alone; the counts are changed by integer atomics, whose
+// order does not matter.
+//
+// The tables are small: what bounds these kernels is latency, so they are few, and one workgroup does
+// what one can. take_kernel ranks the free pages of a chunk of 16,384 and the wanting entries of 1,024
+// sequences by scans in LDS; where there are more of either, count_kernel's sums of each chunk go
+// before, and every workgroup of take_kernel gives away its own chunk's pages. Contents move in units
+// of 16 KB, dealt to a grid that does not know how many there are.
+#include <algorithm>
+
+#include "cache_device.h"
+
+namespace sparsp {
+namespace {
+
+constexpr int kTake = 1024;        // threads of a taking workgroup, and sequences of a chunk
+constexpr int kEach = 16;          // pages of a thread
+constexpr int kChunk = kTake * kEach;
+constexpr int kUnit = kPageUnit;   // bytes of a copying workgroup's turn
+
+// Sum of x over the threads before this one; *all: over all. N threads.
+template <int N>
+__device__ __forceinline__ int scan(int x, int* lds, int* all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = x;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(sum, off);
+        if (lane >= off) sum += y;
+    }
+    __syncthreads();  // the scan before has been read
+    if (lane == 63) lds[wave] = sum;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < N / 64; ++w) {
+        const int y = lds[w];
+        before += w < wave ? y : 0;
+        total += y;
+    }
+    *all = total;
+    return before + sum - x;
+}
+
+__device__ __forceinline__ int tokens_of(const PageArgs& a, int b) {
+    return min(max(a.kv_len[b], 0), a.width * a.page);
+}
+__device__ __forceinline__ bool named(const PageArgs& a, int page) {
+    return page >= 0 && page < a.pages;
+}
+
+// The entries of row b that may want a page.
+struct Range {
+    int begin, count;
+};
+__device__ __forceinline__ Range range_of(const PageArgs& a, int b) {
+    if (b >= a.rows) return {0, 0};
+    const int shift = __builtin_ctz(a.page);
+    if (a.from)  // a fork: the last, partly filled page of a row that has to copy it
+        return {(a.kv_out[b] - 1) >> shift, a.from[b] >= 0 ? 1 : 0};
+    const int kv = tokens_of(a, b);
+    const int n = min(max(a.new_off[b + 1], 0), 1 << 30) - min(max(a.new_off[b], 0), 1 << 30);
+    const int begin = max(kv - n, 0) >> shift;
+    return {begin, n > 0 ? ((kv + a.page - 1) >> shift) - begin : 0};
+}
+
+struct Lds {
+    int sums[kTake / 64];
+    int upto[kTake];  // of the chunk's sequences, the entries before the end of each
+    int begin[kTake];
+};
+
+// Calls give(row, entry, rank) for the wanting entries of the 1,024 sequences from b0 on, rank
+// counted from `rank`; returns how many there are. All threads.
+template <typename Give>
+__device__ __forceinline__ int each_want(const PageArgs& a, int b0, int rank, Lds& l, Give give) {
+    const int t = threadIdx.x;
+    const Range r = range_of(a, b0 + t);
+    int all;
+    const int before = scan<kTake>(r.count, l.sums, &all);
+    l.upto[t] = before + r.count;
+    l.begin[t] = r.begin - before;
+    __syncthreads();
+    int found = 0;
+    for (int e0 = 0; e0 < all; e0 += kTake) {
+        const int e = e0 + t;
+        int s = 0, j = 0;
+        bool want = e < all;
+        if (want) {
+#pragma unroll
+            for (int step = kTake / 2; step; step >>= 1)
+                if (l.upto[s + step - 1] <= e) s += step;
+            j = l.begin[s] + e;
+            want = a.from || !named(a, a.table[int64_t(b0 + s) * a.width + j]);
+        }
+        int sum;
+        const int mine = scan<kTake>(want, l.sums, &sum);
+        if (want) give(b0 + s, j, rank + found + mine);
+        found += sum;
+    }
+    __syncthreads();  // upto and begin have been read
+    return found;
+}
+
+// This thread's pages of a chunk that are free, as bits. What a fork copies from is not, though all
+// that held it may have gone.
+__device__ __forceinline__ uint32_t free_pages(const PageArgs& a, int first) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (first + i < a.pages && a.refs[first + i] <= 0) bits |= 1u << i;
+    if (a.from)
+        for (uint32_t m = bits; m; m &= m - 1)
+            if (a.to[first + __builtin_ctz(m)]) bits &= ~(m & -m);
+    return bits;
+}
+
+// Free pages of each chunk, and behind them wanting entries of each chunk of sequences.
+__global__ __launch_bounds__(kTake) void count_kernel(const PageArgs a, int chunks) {
+    __shared__ Lds l;
+    const int c = blockIdx.x;
+    int all;
+    if (c < chunks)
+        scan<kTake>(__popc(free_pages(a, c * kChunk + threadIdx.x * kEach)), l.sums, &all);
+    else
+        all = each_want(a, (c - chunks) * kTake, 0, l, [](int, int, int) {});
+    if (threadIdx.x == 0) a.counts[c] = all;
+}
+
+// Entry j of row b gets the page of its rank.
+__device__ __forceinline__ void give_page(const PageArgs& a, int b, int j, int rank, int page) {
+    a.table[int64_t(b) * a.width + j] = page;
+    if (a.from) {
+        a.src[rank] = a.from[b];
+        a.dst[rank] = page;
+    }
+}
+
+// All of it, for one chunk of either.
+__global__ __launch_bounds__(kTake) void take_kernel(const PageArgs a) {
+    __shared__ Lds l;
+    __shared__ int list[kChunk];
+    const int first = threadIdx.x * kEach;
+    const uint32_t bits = free_pages(a, first);
+    int all;
+    const int rank = scan<kTake>(__popc(bits), l.sums, &all);
+    for (uint32_t m = bits, r = rank; m; m &= m - 1, ++r) list[r] = first + __builtin_ctz(m);
+    const int wants = each_want(a, 0, 0, l, [](int, int, int) {});
+    if (threadIdx.x == 0) {
+        *a.left = all - wants;
+        if (a.moves) *a.moves = min(all, wants);
+    }
+    for (uint32_t m = bits, r = rank; m && int(r) < wants; m &= m - 1, ++r)
+        a.refs[first + __builtin_ctz(m)] = 1;
+    if (wants > 0)
+        each_want(a, 0, 0, l, [&](int b, int j, int r) {
+            if (r < all) give_page(a, b, j, r, list[r]);
+        });
+}
+
+// The same in two steps for more: the free pages that are taken, in their order, and then each chunk
+// of sequences its own of them. (Not in one, with each chunk of pages looking for the entries that
+// want it: it would meet entries that others have filled already.)
+__global__ __launch_bounds__(kTake) void list_kernel(const PageArgs a, int chunks, int groups) {
+    __shared__ int sums[kTake / 64];
+    const int t = threadIdx.x, c = blockIdx.x;
+    int x = 0, y = 0, z = 0, before, all, wants, mine;
+    for (int k = t; k < chunks; k += kTake) {
+        const int n = a.counts[k];
+        x += k < c ? n : 0;
+        y += n;
+    }
+    for (int k = t; k < groups; k += kTake) z += a.counts[chunks + k];
+    scan<kTake>(x, sums, &before);
+    scan<kTake>(y, sums, &all);
+    scan<kTake>(z, sums, &wants);
+    if (c == 0 && t == 0) {
+        *a.left = all - wants;
+        if (a.moves) *a.moves = min(all, wants);
+    }
+    if (before >= wants) return;
+    const int first = c * kChunk + t * kEach;
+    const uint32_t bits = free_pages(a, first);
+    int r = before + scan<kTake>(__popc(bits), sums, &mine);
+    for (uint32_t m = bits; m && r < wants; m &= m - 1, ++r) {
+        const int page = first + __builtin_ctz(m);
+        a.dst[r] = page;
+        a.refs[page] = 1;
+    }
+}
+__global__ __launch_bounds__(kTake) void give_kernel(const PageArgs a, int chunks) {
+    __shared__ Lds l;
+    const int t = threadIdx.x, g = blockIdx.x;
+    int x = 0, y = 0, rank, all;
+    for (int k = t; k < chunks; k += kTake) y += a.counts[k];
+    for (int k = t; k < g; k += kTake) x += a.counts[chunks + k];
+    scan<kTake>(x, l.sums, &rank);
+    scan<kTake>(y, l.sums, &all);
+    each_want(a, g * kTake, rank, l, [&](int b, int j, int r) {
+        if (r < all) give_page(a, b, j, r, a.dst[r]);
+    });
+}
+
+hipError_t take(const PageArgs& a, hipStream_t s) {
+    const int chunks = (a.pages + kChunk - 1) / kChunk, groups = (a.rows + kTake - 1) / kTake;
+    if (chunks == 1 && groups == 1) {
+        take_kernel<<<1, kTake, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    count_kernel<<<chunks + groups, kTake, 0, s>>>(a, chunks);
+    list_kernel<<<chunks, kTake, 0, s>>>(a, chunks, groups);
+    give_kernel<<<groups, kTake, 0, s>>>(a, chunks);
+    return hipGetLastError();
+}
+
+// Entries whose pages no later token sees are given back.
+__global__ __launch_bounds__(256) void release_kernel(const PageArgs a, int per_row) {
+    const int b = blockIdx.x / per_row;
+    const int kv = tokens_of(a, b);
+    for (int j = blockIdx.x % per_row * 256 + threadIdx.x; j < a.width; j += per_row * 256) {
+        const int64_t begin = int64_t(j) * a.page;
+        const bool slid = a.window > 0 && begin >= a.sinks &&
+                          begin + a.page <= int64_t(kv) - a.window + 1;
+        if (begin < kv && !slid) continue;
+        int32_t* at = a.table + int64_t(b) * a.width + j;
+        const int page = *at;
+        if (named(a, page)) atomicSub(a.refs + page, 1);
+        *at = -1;
+    }
+}
+
+// The rows of the new table; and the counts as they were, for fork_counts_kernel to change.
+__global__ __launch_bounds__(256) void fork_rows_kernel(const PageArgs a) {
+    const int i = blockIdx.x, t = threadIdx.x;
+    if (i >= a.rows) {
+        const int at = (i - a.rows) * 1024 + t * 4;
+        for (int e = at; e < min(at + 4, a.pages); ++e) {
+            a.refs[e] = a.old_refs[e];
+            a.to[e] = 0;
+        }
+        return;
+    }
+    const int p = a.parents[i];
+    const bool live = p >= 0 && p < a.old_rows;
+    const int kv = live ? tokens_of(a, p) : 0;
+    const int need = (kv + a.page - 1) / a.page;
+    bool other = false;  // an earlier row continues the same one
+    for (int k = t; k < i; k += 256) other |= a.parents[k] == p;
+    other = __syncthreads_or(other);
+    const int32_t* old = a.old_table + int64_t(live ? p : 0) * a.width;
+    for (int j = t; j < a.width; j += 256) {
+        int page = j < need ? old[j] : -1;
+        if (!named(a, page)) page = -1;
+        if (j == need - 1) {
+            // A page that is not full goes to the first row, if nothing else holds it.
+            const bool copy = page >= 0 && kv % a.page && (other || a.old_refs[page] != 1);
+            a.from[i] = copy ? page : -1;
+            if (copy) page = -1;
+        }
+        a.table[int64_t(i) * a.width + j] = page;
+    }
+    if (t == 0) {
+        a.kv_out[i] = kv;
+        if (need == 0) a.from[i] = -1;
+    }
+}
+
+// What each old row's entries come to: one for each row that continues it, less its own.
+__global__ __launch_bounds__(256) void fork_counts_kernel(const PageArgs a) {
+    __shared__ int sums[4];
+    const int p = blockIdx.x, t = threadIdx.x;
+    int children = 0;
+    for (int k = t; k < a.rows; k += 256) children += a.parents[k] == p;
+    scan<256>(children, sums, &children);
+    const int kv = tokens_of(a, p);
+    for (int j = t; j < a.width; j += 256) {
+        const int page = a.old_table[int64_t(p) * a.width + j];
+        if (!named(a, page)) continue;
+        const int64_t begin = int64_t(j) * a.page;
+        int delta = -1;
+        if (begin + a.page <= kv)
+            delta = children - 1;
+        else if (begin < kv && children > 0) {
+            if (a.old_refs[page] == 1)
+                delta = 0;
+            else
+                a.to[page] = 1;  // copied for every row
+        }
+        if (delta) atomicAdd(a.refs + page, delta);
+    }
+}
+
+// One unit of the pages' contents: 16 KB of page `src` of one buffer to page `dst`.
+__device__ __forceinline__ void copy_unit(const PageBuffers& f, int src, int dst, int u) {
+    int n = 0;
+    while (n + 1 < f.count && u >= f.first[n + 1]) ++n;
+    const int64_t bytes = f.bytes[n], at = int64_t(u - f.first[n]) * kUnit;
+    const char* from = f.data[n] + src * bytes + at;
+    char* to = f.data[n] + dst * bytes + at;
+    uint4 x[kUnit / 4096];
+#pragma unroll
+    for (int k = 0; k < kUnit / 4096; ++k) {
+        const int off = k * 4096 + threadIdx.x * 16;
+        if (at + off < bytes) x[k] = load_nt(from + off);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnit / 4096; ++k) {
+        const int off = k * 4096 + threadIdx.x * 16;
+        if (at + off < bytes) store_nt(to + off, x[k]);
+    }
+}
+
+// Pages src[k] to dst[k], k below *moves (or `most`, where that is NULL).
+__global__ __launch_bounds__(256) void copy_kernel(const PageBuffers f, const int32_t* src,
+                                                   const int32_t* dst, const int32_t* moves, int most,
+                                                   int pages) {
+    const int64_t units = int64_t(moves ? *moves : most) * f.units;
+    for (int64_t w = blockIdx.x; w < units; w += gridDim.x) {
+        const int k = int(w / f.units);
+        const int s = src[k], d = dst[k];
+        if (s < 0 || s >= pages || d < 0 || d >= pages || s == d) continue;
+        copy_unit(f, s, d, int(w % f.units));
+    }
+}
+
+// This thread's pages of a chunk that are in use, as bits.
+__device__ __forceinline__ uint32_t used_pages(const PageArgs& a, int first) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (first + i < a.pages && a.old_refs[first + i] > 0) bits |= 1u << i;
+    return bits;
+}
+__global__ __launch_bounds__(kTake) void used_kernel(const PageArgs a) {
+    __shared__ int sums[kTake / 64];
+    int all;
+    scan<kTake>(__popc(used_pages(a, blockIdx.x * kChunk + threadIdx.x * kEach)), sums, &all);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = all;
+}
+
+// With n pages in use, the k-th page in use from n on goes to the k-th free one below n: dst[k]. Of
+// the pages in use from n on, src counts from the last, since that needs no count of those below n;
+// to[page] is that number. *moves is how many there are. The counts of the pages below n that stay.
+__global__ __launch_bounds__(kTake) void compact_kernel(const PageArgs a, int chunks) {
+    __shared__ int sums[kTake / 64];
+    const int t = threadIdx.x, c = blockIdx.x, first = c * kChunk + t * kEach;
+    const uint32_t used = used_pages(a, first);
+    int mine, before = 0;
+    int rank = scan<kTake>(__popc(used), sums, &mine);
+    int n = mine;
+    if (chunks > 1) {
+        int x = 0, y = 0;
+        for (int k = t; k < chunks; k += kTake) {
+            const int m = a.counts[k];
+            x += k < c ? m : 0;
+            y += m;
+        }
+        scan<kTake>(x, sums, &before);
+        scan<kTake>(y, sums, &n);
+    }
+    rank += before;  // pages in use before this thread's
+    if (c == 0 && t == 0) {
+        *a.left = n;
+        if (n == a.pages) *a.moves = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int p = first + i;
+        if (p >= a.pages) break;
+        const bool in_use = used >> i & 1;
+        if (p == n) *a.moves = n - rank;
+        if (p < n) {
+            if (!in_use) a.dst[p - rank] = p;
+        } else if (in_use) {
+            a.src[n - 1 - rank] = p;
+            a.to[p] = n - 1 - rank;
+        }
+        if (p >= n || in_use) a.refs[p] = p < n ? a.old_refs[p] : 0;
+        rank += in_use;
+    }
+}
+
+// The first workgroups rewrite the table, the others move contents and counts.
+__global__ __launch_bounds__(256) void compact_move_kernel(const PageArgs a, const PageBuffers f,
+                                                           int tables) {
+    const int moves = *a.moves, n = *a.left;
+    if (int(blockIdx.x) < tables) {
+        const int64_t entries = int64_t(a.rows) * a.width;
+        for (int64_t e = blockIdx.x * 256 + threadIdx.x; e < entries; e += tables * 256) {
+            int page = a.old_table[e];
+            if (!named(a, page) || a.old_refs[page] <= 0)
+                page = -1;
+            else if (page >= n)
+                page = a.dst[moves - 1 - a.to[page]];
+            a.table[e] = page;
+        }
+        return;
+    }
+    const int each = max(f.units, 1);  // (no contents: the counts alone)
+    const int64_t units = int64_t(moves) * each;
+    for (int64_t w = blockIdx.x - tables; w < units; w += gridDim.x - tables) {
+        const int k = int(w / each), u = int(w % each);
+        const int src = a.src[moves - 1 - k], dst = a.dst[k];
+        if (u == 0 && threadIdx.x == 0) a.refs[dst] = a.old_refs[src];
+        if (f.units > 0) copy_unit(f, src, dst, u);
+    }
+}
+
+int copy_grid(int64_t units) {
+    return int(std::min<int64_t>(std::max<int64_t>(units, 1), 8 * 256));
+}
+
+}  // namespace
+
+hipError_t launch_pages_reserve(const PageArgs& a, hipStream_t s) { return take(a, s); }
+
+hipError_t launch_pages_release(const PageArgs& a, hipStream_t s) {
+    const int per_row = std::min((a.width + 255) / 256, 16);
+    release_kernel<<<a.rows * per_row, 256, 0, s>>>(a, per_row);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PageArgs& a, const PageBuffers& f, hipStream_t s) {
+    fork_rows_kernel<<<a.rows + (a.pages + 1023) / 1024, 256, 0, s>>>(a);
+    fork_counts_kernel<<<a.old_rows, 256, 0, s>>>(a);
+    const hipError_t e = take(a, s);
+    if (e != hipSuccess || f.count == 0) return e;
+    copy_kernel<<<copy_grid(int64_t(a.rows) * f.units), 256, 0, s>>>(f, a.src, a.dst, a.moves, 0,
+                                                                     a.pages);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const PageBuffers& f, const int32_t* src, const int32_t* dst, int count,
+                             int pages, hipStream_t s) {
+    copy_kernel<<<copy_grid(int64_t(count) * f.units), 256, 0, s>>>(f, src, dst, nullptr, count, pages);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PageArgs& a, const PageBuffers& f, hipStream_t s) {
+    const int chunks = (a.pages + kChunk - 1) / kChunk;
+    if (chunks > 1) used_kernel<<<chunks, kTake, 0, s>>>(a);
+    compact_kernel<<<chunks, kTake, 0, s>>>(a, chunks);
+    const int tables = int(std::min<int64_t>((int64_t(a.rows) * a.width + 255) / 256, 256));
+    compact_move_kernel<<<tables + copy_grid(int64_t(a.pages / 2) * std::max(f.units, 1)), 256, 0, s>>>(
+        a, f, tables);
+    return hipGetLastError();
+}
+
+}  // namespace sparsp

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2609_32197_amd as sp
-from paper_2609_32197_amd.bounded import _CACHE4
+from paper_2609_32197_amd.bounded import _BUFFER, _CACHE4, _PAGES
 from paper_2609_32197_amd.paged import _CACHE, _ROWS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -201,3 +201,92 @@ def test_binding_of_the_4_bit_cache_wants_the_gpu():
         sp.sparsp_paged_attn4(x, c.K, i, off, kv)
     with pytest.raises(ValueError):
         sp.Cache4.zeros(4, 2, 16, 48, device="cpu")
+
+
+# ---------------------------------------------------------------------------
+# pages
+# ---------------------------------------------------------------------------
+
+
+def pages(**kw):
+    v = dict(refs=AT, table=2 * AT, kv_len=3 * AT, pages=9, page=16, width=4, B=3)
+    v.update(kw)
+    return _PAGES.pack(*v.values())
+
+
+def buffers(*pairs):
+    return b"".join(_BUFFER.pack(*x) for x in pairs)
+
+
+def fork(p=None, parents=AT, n=3, b=buffers((AT, 64)), count=1, out=(4 * AT, 5 * AT, 6 * AT, 7 * AT),
+         ws=8 * AT, nbytes=1 << 20):
+    return sp.load_library().sparsp_pages_fork(p or pages(), parents, n, b, count, *out, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(p=pages(refs=0)), "SPARSP_E_INVALID", "NULL"),
+    (dict(p=pages(kv_len=0)), "SPARSP_E_INVALID", "NULL"),
+    (dict(p=pages(pages=0)), "SPARSP_E_INVALID", "positive"),
+    (dict(p=pages(page=48)), "SPARSP_E_UNSUPPORTED", "page"),
+    (dict(p=pages(width=1 << 27)), "SPARSP_E_UNSUPPORTED", "2^30"),
+    (dict(p=pages(width=1 << 16, B=1 << 15)), "SPARSP_E_UNSUPPORTED", "2^30"),
+    (dict(parents=0), "SPARSP_E_INVALID", "NULL"),
+    (dict(n=0), "SPARSP_E_UNSUPPORTED", "rows"),
+    (dict(n=65537), "SPARSP_E_UNSUPPORTED", "rows"),
+    (dict(count=9), "SPARSP_E_INVALID", "buffers"),
+    (dict(b=None), "SPARSP_E_INVALID", "buffers"),
+    (dict(b=buffers((AT, 24))), "SPARSP_E_INVALID", "multiple of 16"),
+    (dict(b=buffers((AT, 0))), "SPARSP_E_INVALID", "multiple of 16"),
+    (dict(b=buffers((AT + 4, 32))), "SPARSP_E_INVALID", "aligned"),
+    (dict(b=buffers((AT, 32), (2 * AT, 32), (AT, 32)), count=3), "SPARSP_E_INVALID", "same memory"),
+    (dict(out=(2 * AT, 5 * AT, 6 * AT, 7 * AT)), "SPARSP_E_INVALID", "inputs"),
+    (dict(out=(4 * AT, 3 * AT, 6 * AT, 7 * AT)), "SPARSP_E_INVALID", "inputs"),
+    (dict(out=(4 * AT, 5 * AT, AT, 7 * AT)), "SPARSP_E_INVALID", "inputs"),
+    (dict(out=(4 * AT, 5 * AT, 6 * AT, 0)), "SPARSP_E_INVALID", "NULL"),
+    (dict(ws=0), "SPARSP_E_INVALID", "workspace"),
+    (dict(nbytes=100), "SPARSP_E_CAPACITY", "workspace"),
+])
+def test_fork_refused(kw, code, word):
+    got, message = status(fork(**kw))
+    assert got == code and word in message
+
+
+def test_other_page_calls_refused():
+    lib = sp.load_library()
+    for call, word in (
+            (lambda: lib.sparsp_pages_reserve(pages(), 0, AT, AT, 1 << 20, None), "NULL"),
+            (lambda: lib.sparsp_pages_reserve(pages(), AT, 0, AT, 1 << 20, None), "NULL"),
+            (lambda: lib.sparsp_pages_reserve(pages(), AT, AT, AT, 8, None), "workspace"),
+            (lambda: lib.sparsp_pages_release(pages(), -1, 0, None), "window"),
+            (lambda: lib.sparsp_pages_release(pages(), 0, 4, None), "sinks"),
+            (lambda: lib.sparsp_pages_compact(pages(), None, 0, 2 * AT, 5 * AT, 6 * AT, AT, 1 << 20, None),
+             "inputs"),
+            (lambda: lib.sparsp_pages_compact(pages(), None, 0, 4 * AT, 5 * AT, 0, AT, 1 << 20, None), "NULL"),
+            (lambda: lib.sparsp_pages_copy(buffers((AT, 16)), 0, 9, AT, AT, 3, None), "nothing"),
+            (lambda: lib.sparsp_pages_copy(buffers((AT, 16)), 1, 0, AT, AT, 3, None), "pages"),
+            (lambda: lib.sparsp_pages_copy(buffers((AT, 16)), 1, 9, AT, AT, -1, None), "moves"),
+            (lambda: lib.sparsp_pages_copy(buffers((AT, 16)), 1, 9, 0, AT, 3, None), "NULL"),
+            (lambda: lib.sparsp_pages_workspace_bytes(pages(page=8), 0), "page"),
+            (lambda: lib.sparsp_pages_workspace_bytes(pages(), -1), "rows")):
+        assert word in status(call())[1]
+    assert lib.sparsp_pages_copy(buffers((AT, 16)), 1, 9, 0, 0, 0, None) == 0
+
+
+def test_page_workspace_holds_its_lists():
+    """counts, three lists of pages and one of rows, each on 4 bytes."""
+    refs, table = torch.zeros(20000, dtype=torch.int32), torch.zeros(5, 7, dtype=torch.int32)
+    for rows_ in (0, 5, 3000):
+        n = sp.sparsp_pages_workspace_bytes(refs, table, rows_)
+        assert n >= 4 * (3 * 20000 + max(rows_, 5) + 2 + -(-max(rows_, 5) // 1024) + 1)
+
+
+def test_page_calls_want_the_gpu():
+    i = torch.zeros(9, dtype=torch.int32)
+    t, kv = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: sp.sparsp_pages_reserve(i, t, i[:3], kv, 16),
+                 lambda: sp.sparsp_pages_release(i, t, kv, 16),
+                 lambda: sp.sparsp_pages_fork(i, t, kv, kv, 16),
+                 lambda: sp.sparsp_pages_compact(i, t),
+                 lambda: sp.sparsp_pages_copy(kv, kv, torch.zeros(9, 8))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
