@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "paged_four.h"
+#include "paged_tiles.h"
 
 namespace sparsp {
 namespace {
@@ -52,6 +52,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     // Entries of the page list: pages, or with a window 16 keys each (the gap is no multiple of
     // a page).
     const int list_shift = WINDOW ? 4 : shift;
+
 
     for (int tile = work.tile; tile * int64_t(16 * NC) < rows; tile += work.stride) {
         if constexpr (WINDOW) {
@@ -105,11 +106,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
         };
         auto load_k = [&](Stage& st, int t0, int p0) {
             st.kp = page_list[((t0 + M::k_group(lane)) >> list_shift) - p0];
-            M::load_k(M::source(a), st.k, st.kp, hk, WINDOW ? span.cached(t0) : t0, lane);
+            M::load_k(c, st.k, st.kp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         auto load_v = [&](Stage& st, int t0, int p0) {
             st.vp = page_list[((t0 + M::v_group(lane)) >> list_shift) - p0];
-            M::load_v(M::source(a), st.v, st.vp, hk, WINDOW ? span.cached(t0) : t0, lane);
+            M::load_v(c, st.v, st.vp, hk, WINDOW ? span.cached(t0) : t0, lane);
         };
         // after_scores: what is done once K has been used.
         auto compute = [&](Stage& st, int t0, auto after_scores) {
@@ -402,6 +403,8 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     Shape r = {};
     const int64_t rows = int64_t(most_new) * G;
     r.rows = rows <= 16 ? 16 : c.dtype == SPARSP_F32 || (rows <= 32 && c.d <= 64) ? 32 : 128;
+    // (three terms of 32 rows do not fit into the registers at d > 64)
+    if (a.k_scales && c.dtype == SPARSP_F32 && c.d > 64) r.rows = 16;
     r.plan.rows = r.rows;
     r.plan.grain = r.rows == 128 ? 64 : c.dtype == SPARSP_F32 && !a.k_scales ? 16 : 32;
     if (a.window) {  // (the most that a tile's Span is long)
@@ -464,17 +467,7 @@ hipError_t launch_rows(const PagedArgs& a, const PagedPlan& p, hipStream_t s) {
 
 hipError_t launch_few(const PagedArgs& a, const Shape& r, hipStream_t s) {
     const bool small = a.cache.d <= 64, few = r.rows == 16;
-    if (a.k_scales) {
-        if (a.cache.dtype == SPARSP_BF16)
-            return !small ? launch_rows<Four<1>, 128, 1>(a, r.plan, s)
-                   : few  ? launch_rows<Four<1>, 64, 1>(a, r.plan, s)
-                          : launch_rows<Four<1>, 64, 2>(a, r.plan, s);
-        if (few)
-            return small ? launch_rows<Four<3>, 64, 1>(a, r.plan, s)
-                         : launch_rows<Four<3>, 128, 1>(a, r.plan, s);
-        return small ? launch_rows<Four<3>, 64, 2>(a, r.plan, s)
-                     : launch_rows<Four<3>, 128, 2>(a, r.plan, s);
-    }
+    if (a.k_scales) return launch_four_few(a, r.plan, s);
     if (a.cache.dtype == SPARSP_BF16)
         return !small ? launch_rows<uint16_t, 128, 1>(a, r.plan, s)
                : few  ? launch_rows<uint16_t, 64, 1>(a, r.plan, s)

@@ -21,6 +21,8 @@ struct PagedPlan {
 
 // Row tiles of 128 on LDS tiles, bf16 (paged_attn_tiles.hip).
 hipError_t launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, hipStream_t s);
+// Few rows a sequence over a cache held in 4 bits (paged_attn4.hip).
+hipError_t launch_four_few(const PagedArgs& a, const PagedPlan& p, hipStream_t s);
 // Weights of 256 keys a workgroup with Q through LDS, bf16 (paged_weights_tiles.hip).
 hipError_t launch_weights_tiles(const PagedArgs& a, hipStream_t s);
 

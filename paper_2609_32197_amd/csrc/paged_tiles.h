@@ -44,7 +44,6 @@ struct TileMath<uint16_t, D> {
     struct QTile { bf16x8 q[KT]; };
     struct VTile { uint32_t r[8][DV / 2]; };
 
-    static __device__ __forceinline__ const sparsp_cache& source(const PagedArgs& a) { return a.cache; }
     static __device__ __forceinline__ int key_of(int g, int v) { return 8 * g + v; }
     static __device__ __forceinline__ int k_group(int lane) { return 8 * ((lane & 15) >> 2); }
     static __device__ __forceinline__ int v_group(int lane) { return 8 * (lane >> 4); }
@@ -153,7 +152,6 @@ struct TileMath<float, D> {
     struct QTile { floatx4 q[KT]; };
     struct VTile { float r[4][DV]; };
 
-    static __device__ __forceinline__ const sparsp_cache& source(const PagedArgs& a) { return a.cache; }
     static __device__ __forceinline__ int key_of(int g, int v) { return 4 * g + v; }
     static __device__ __forceinline__ int k_group(int) { return 0; }
     static __device__ __forceinline__ int v_group(int lane) { return 4 * (lane >> 4); }
