@@ -433,6 +433,10 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
         parts = std::max(fill, std::min(level, (rounds + least - 1) / least));
         if (tall && (live > 2 * kCus || parts < 2 * fill)) parts = fill;
         parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
+        // Where a window bounds the longest sequences, those that reach it are many and end together
+        // (64 sequences of 400 to 32,768, one new token each: window 2,048 85 us whole, 98 us in 2
+        // parts; 4,096 142 and 154; 8,192 239 whole, 224 in 5).
+        if (a.window && !tall && fill == 1 && rounds * round <= 5120) parts = 1;
     }
     const int64_t all_rows = int64_t(a.q_heads) * a.tokens, part_bytes = all_rows * (c.d + 2) * 4;
     parts = std::max<int64_t>(1, std::min(parts, ws_bytes / part_bytes));
