@@ -64,37 +64,52 @@ __device__ __forceinline__ Vec<T, V> get(const char* row, int ch) {
     return *reinterpret_cast<const Vec<T, V>*>(row + ch * int(sizeof(T)));
 }
 
-// Codes of eight channels and the scale's exponent byte, which the four lanes of a group share.
-__device__ __forceinline__ uint32_t magnitude(double y) {  // grows with |y|; its exponent from bit 20
-    return uint32_t(__double2hiint(y)) & 0x7fffffffu;
-}
-template <typename Y>
-__device__ __forceinline__ uint32_t quantise(const Y (&y)[8], uint32_t* scale) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, magnitude(double(y[e])));
+// Codes of eight channels and the scale's exponent byte, which the four lanes of a group share. top:
+// the largest magnitude's bits, with the exponent (of a float64) from bit `at` on; an infinity or a
+// NaN gets the scale that stands for NaN.
+template <int AT, int BIAS>
+__device__ __forceinline__ int group_exponent(uint32_t top, uint32_t* scale) {
     top = max(top, uint32_t(__shfl_xor(int(top), 1)));
     top = max(top, uint32_t(__shfl_xor(int(top), 2)));
-    if (top >= 0x7ff00000u) {  // an infinity or a NaN: the scale that stands for NaN
-        *scale = 255;
-        return 0;
-    }
-    const int exponent = min(max(int(top >> 20) - 1023 - 2, -125), 125);
-    *scale = uint32_t(exponent + 127);
-    const Y unit = Y(__uint_as_float(uint32_t(127 - exponent) << 23));
-    uint32_t codes = 0;
+    const int e = min(max(int(top >> AT) - BIAS - 2, -125), 125);
+    *scale = int(top >> AT) > 2 * BIAS ? 255u : uint32_t(e + 127);
+    return e;
+}
+// The conversion divides by the scale, rounds to the nearest code, ties to the even one, and cuts to 6.
+__device__ __forceinline__ uint32_t codes_of(const float (&y)[8], float scale) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+}
+__device__ __forceinline__ uint32_t quantise(const float (&y)[8], uint32_t* scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+    const int exponent = group_exponent<23, 127>(top, scale);
+    const uint32_t codes = codes_of(y, __uint_as_float(uint32_t(exponent + 127) << 23));
+    return *scale == 255 ? 0u : codes;
+}
+// A float64 over 2^e is cut to float32, with the last bit set if that leaves anything out: such a
+// number is on the same side of every border as the float64. (Borders have few bits; what is below
+// 2^-126 of the scale becomes 0.)
+__device__ __forceinline__ uint32_t quantise(const double (&y)[8], uint32_t* scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, uint32_t(__double2hiint(y[e])) & 0x7fffffffu);
+    const int exponent = group_exponent<20, 1023>(top, scale);
+    const int shift = (1023 - 127 + exponent) << 20;
+    float m[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const Y a = y[e] < 0 ? -y[e] : y[e], m = a * unit;
-        // Steps of a half below 2, of one below 4, of two from there.
-        const Y step = m < 2 ? Y(2) : m < 4 ? Y(1) : Y(0.5);
-        const int base = m < 2 ? 0 : m < 4 ? 2 : 4;
-        const int code = min(int(rint(m * step)) + base, 7);
-        const bool sign = sizeof(Y) == 8 ? __double2hiint(double(y[e])) < 0
-                                         : int(__float_as_uint(float(y[e]))) < 0;
-        codes |= uint32_t(code | (sign ? 8 : 0)) << (4 * e);
+        const uint32_t hi = uint32_t(__double2hiint(y[e])), lo = uint32_t(__double2loint(y[e]));
+        const int high = max(int(hi & 0x7fffffffu) - shift, 0);  // exponent in place, 20 bits behind it
+        const uint32_t left = min(lo & 0x1fffffffu, 1u);
+        m[e] = __uint_as_float((hi & 0x80000000u) | __builtin_amdgcn_alignbit(high, lo, 29) | left);
     }
-    return codes;
+    const uint32_t codes = codes_of(m, 1.f);
+    return *scale == 255 ? 0u : codes;
 }
 
 template <typename T, int V, bool HALF>

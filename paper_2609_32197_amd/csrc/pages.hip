@@ -6,10 +6,12 @@
 // order does not matter.
 //
 // The tables are small: what bounds these kernels is latency, so they are few, and one workgroup does
-// what one can. take_kernel ranks the free pages of a chunk of 16,384 and the wanting entries of 1,024
-// sequences by scans in LDS; where there are more of either, count_kernel's sums of each chunk go
-// before, and every workgroup of take_kernel gives away its own chunk's pages. Contents move in units
-// of 16 KB, dealt to a grid that does not know how many there are.
+// what one can. take_kernel ranks the free pages and the wanting entries of 1,024 sequences at a time
+// by scans, a thread 16 to 64 pages in a row, in loads of four. For more pages than that or many
+// sequences, count_kernel's sums of each chunk go before, list_kernel lists the pages that are
+// taken, and give_kernel's workgroups give them to a chunk of sequences each (512 sequences, 19,800
+// pages: 27 us, one workgroup TAKE us). Contents move in units of 16 KB, dealt to a grid that does not
+// know how many there are.
 #include <algorithm>
 
 #include "cache_device.h"
@@ -17,10 +19,11 @@
 namespace sparsp {
 namespace {
 
-constexpr int kTake = 1024;        // threads of a taking workgroup, and sequences of a chunk
-constexpr int kEach = 16;          // pages of a thread
+constexpr int kTake = 1024;       // threads of a taking workgroup, and sequences of a chunk
+constexpr int kEach = 16;         // pages of a thread and chunk
 constexpr int kChunk = kTake * kEach;
-constexpr int kUnit = kPageUnit;   // bytes of a copying workgroup's turn
+constexpr int kAlone = 4;         // chunks that one workgroup takes from
+constexpr int kUnit = kPageUnit;  // bytes of a copying workgroup's turn
 
 // Sum of x over the threads before this one; *all: over all. N threads.
 template <int N>
@@ -106,26 +109,60 @@ __device__ __forceinline__ int each_want(const PageArgs& a, int b0, int rank, Ld
     return found;
 }
 
-// This thread's pages of a chunk that are free, as bits. What a fork copies from is not, though all
-// that held it may have gone.
-__device__ __forceinline__ uint32_t free_pages(const PageArgs& a, int first) {
-    uint32_t bits = 0;
+// Four numbers of x from 4 i on, of `count` in all; `fill` behind them.
+__device__ __forceinline__ int4 four_of(const int32_t* x, int i, int count, int fill) {
+    const int at = 4 * i;
+    if (at + 4 <= count && (reinterpret_cast<uintptr_t>(x) & 15) == 0)
+        return *reinterpret_cast<const int4*>(x + at);
+    return make_int4(at < count ? x[at] : fill, at + 1 < count ? x[at + 1] : fill,
+                     at + 2 < count ? x[at + 2] : fill, at + 3 < count ? x[at + 3] : fill);
+}
+
+// The pages of a workgroup, kTake * N * kEach from `base` on: which of them are free (or in use), as
+// bits of the thread that has N * kEach in a row. They are loaded four a thread as they lie (the
+// sixteen of a thread at once would be as many cache lines a load as it has lanes: 31,000 pages and
+// what a fork copies from, 21 us) and change hands in LDS.
+template <int N>
+struct PageBits {
+    uint8_t quads[kTake * N * kEach / 4];
+};
+template <int N, typename Test>
+__device__ __forceinline__ uint64_t page_bits(PageBits<N>& lds, int base, Test test) {
+    const int t = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        if (first + i < a.pages && a.refs[first + i] <= 0) bits |= 1u << i;
-    if (a.from)
-        for (uint32_t m = bits; m; m &= m - 1)
-            if (a.to[first + __builtin_ctz(m)]) bits &= ~(m & -m);
+    for (int k = 0; k < N * kEach / 4; ++k) lds.quads[k * kTake + t] = test(base / 4 + k * kTake + t);
+    __syncthreads();
+    uint64_t bits = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        uint32_t q = reinterpret_cast<const uint32_t*>(lds.quads)[t * N + n];  // a nibble a byte
+        q = (q | q >> 4) & 0x00ff00ffu;
+        bits |= uint64_t((q | q >> 8) & 0xffffu) << (n * kEach);
+    }
     return bits;
+}
+// Free ones. What a fork copies from is not, though all that held it may have gone.
+template <int N>
+__device__ __forceinline__ uint64_t free_pages(const PageArgs& a, PageBits<N>& lds, int base) {
+    return page_bits<N>(lds, base, [&](int i) {
+        const int4 x = four_of(a.refs, i, a.pages, 1);
+        int free = (x.x <= 0) | (x.y <= 0) << 1 | (x.z <= 0) << 2 | (x.w <= 0) << 3;
+        if (a.from) {
+            const int4 y = four_of(a.to, i, a.pages, 0);
+            free &= (y.x == 0) | (y.y == 0) << 1 | (y.z == 0) << 2 | (y.w == 0) << 3;
+        }
+        return uint8_t(free);
+    });
 }
 
 // Free pages of each chunk, and behind them wanting entries of each chunk of sequences.
 __global__ __launch_bounds__(kTake) void count_kernel(const PageArgs a, int chunks) {
     __shared__ Lds l;
+    __shared__ PageBits<1> pages;
     const int c = blockIdx.x;
     int all;
     if (c < chunks)
-        scan<kTake>(__popc(free_pages(a, c * kChunk + threadIdx.x * kEach)), l.sums, &all);
+        scan<kTake>(__popcll(free_pages<1>(a, pages, c * kChunk)), l.sums, &all);
     else
         all = each_want(a, (c - chunks) * kTake, 0, l, [](int, int, int) {});
     if (threadIdx.x == 0) a.counts[c] = all;
@@ -140,26 +177,51 @@ __device__ __forceinline__ void give_page(const PageArgs& a, int b, int j, int r
     }
 }
 
-// All of it, for one chunk of either.
-__global__ __launch_bounds__(kTake) void take_kernel(const PageArgs a) {
+// The number of x's set bit that has k others below it.
+__device__ __forceinline__ int bit_of(uint64_t x, int k) {
+    int at = 0;
+#pragma unroll
+    for (int w = 32; w; w >>= 1) {
+        const int below = __popcll(x >> at & ((uint64_t(1) << w) - 1));
+        if (k >= below) {
+            k -= below;
+            at += w;
+        }
+    }
+    return at;
+}
+
+// All of it by one workgroup, of N chunks of pages. An entry finds its page by its rank among the
+// threads' free pages, so nothing is listed.
+template <int N>
+__global__ __launch_bounds__(kTake) void take_kernel(const PageArgs a, int groups) {
     __shared__ Lds l;
-    __shared__ int list[kChunk];
-    const int first = threadIdx.x * kEach;
-    const uint32_t bits = free_pages(a, first);
+    __shared__ PageBits<N> pages;
+    __shared__ uint64_t free[kTake];
+    __shared__ int upto[kTake];
+    const int t = threadIdx.x;
+    const uint64_t bits = free_pages<N>(a, pages, 0);
     int all;
-    const int rank = scan<kTake>(__popc(bits), l.sums, &all);
-    for (uint32_t m = bits, r = rank; m; m &= m - 1, ++r) list[r] = first + __builtin_ctz(m);
-    const int wants = each_want(a, 0, 0, l, [](int, int, int) {});
-    if (threadIdx.x == 0) {
+    const int rank = scan<kTake>(__popcll(bits), l.sums, &all);
+    free[t] = bits;
+    upto[t] = rank + __popcll(bits);
+    int wants = 0;  // (each_want begins with a barrier)
+    for (int g = 0; g < groups; ++g)
+        wants += each_want(a, g * kTake, wants, l, [&](int b, int j, int r) {
+            if (r >= all) return;
+            int s = 0;
+#pragma unroll
+            for (int step = kTake / 2; step; step >>= 1)
+                if (upto[s + step - 1] <= r) s += step;
+            const uint64_t x = free[s];
+            const int page = s * N * kEach + bit_of(x, r - upto[s] + __popcll(x));
+            a.refs[page] = 1;
+            give_page(a, b, j, r, page);
+        });
+    if (t == 0) {
         *a.left = all - wants;
         if (a.moves) *a.moves = min(all, wants);
     }
-    for (uint32_t m = bits, r = rank; m && int(r) < wants; m &= m - 1, ++r)
-        a.refs[first + __builtin_ctz(m)] = 1;
-    if (wants > 0)
-        each_want(a, 0, 0, l, [&](int b, int j, int r) {
-            if (r < all) give_page(a, b, j, r, list[r]);
-        });
 }
 
 // The same in two steps for more: the free pages that are taken, in their order, and then each chunk
@@ -167,6 +229,7 @@ __global__ __launch_bounds__(kTake) void take_kernel(const PageArgs a) {
 // want it: it would meet entries that others have filled already.)
 __global__ __launch_bounds__(kTake) void list_kernel(const PageArgs a, int chunks, int groups) {
     __shared__ int sums[kTake / 64];
+    __shared__ PageBits<1> pages;
     const int t = threadIdx.x, c = blockIdx.x;
     int x = 0, y = 0, z = 0, before, all, wants, mine;
     for (int k = t; k < chunks; k += kTake) {
@@ -184,7 +247,7 @@ __global__ __launch_bounds__(kTake) void list_kernel(const PageArgs a, int chunk
     }
     if (before >= wants) return;
     const int first = c * kChunk + t * kEach;
-    const uint32_t bits = free_pages(a, first);
+    const uint32_t bits = uint32_t(free_pages<1>(a, pages, c * kChunk));
     int r = before + scan<kTake>(__popc(bits), sums, &mine);
     for (uint32_t m = bits; m && r < wants; m &= m - 1, ++r) {
         const int page = first + __builtin_ctz(m);
@@ -207,8 +270,9 @@ __global__ __launch_bounds__(kTake) void give_kernel(const PageArgs a, int chunk
 
 hipError_t take(const PageArgs& a, hipStream_t s) {
     const int chunks = (a.pages + kChunk - 1) / kChunk, groups = (a.rows + kTake - 1) / kTake;
-    if (chunks == 1 && groups == 1) {
-        take_kernel<<<1, kTake, 0, s>>>(a);
+    if (chunks <= kAlone && groups <= 4) {
+        const auto kernel = chunks == 1 ? take_kernel<1> : chunks == 2 ? take_kernel<2> : take_kernel<4>;
+        kernel<<<1, kTake, 0, s>>>(a, groups);
         return hipGetLastError();
     }
     count_kernel<<<chunks + groups, kTake, 0, s>>>(a, chunks);
@@ -327,18 +391,17 @@ __global__ __launch_bounds__(256) void copy_kernel(const PageBuffers f, const in
     }
 }
 
-// This thread's pages of a chunk that are in use, as bits.
-__device__ __forceinline__ uint32_t used_pages(const PageArgs& a, int first) {
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        if (first + i < a.pages && a.old_refs[first + i] > 0) bits |= 1u << i;
-    return bits;
+__device__ __forceinline__ uint8_t in_use(int4 x) {
+    return uint8_t((x.x > 0) | (x.y > 0) << 1 | (x.z > 0) << 2 | (x.w > 0) << 3);
 }
 __global__ __launch_bounds__(kTake) void used_kernel(const PageArgs a) {
     __shared__ int sums[kTake / 64];
-    int all;
-    scan<kTake>(__popc(used_pages(a, blockIdx.x * kChunk + threadIdx.x * kEach)), sums, &all);
+    int used = 0, all;
+#pragma unroll
+    for (int k = 0; k < kEach / 4; ++k)
+        used += __popc(in_use(four_of(
+            a.old_refs, blockIdx.x * (kChunk / 4) + k * kTake + threadIdx.x, a.pages, 0)));
+    scan<kTake>(used, sums, &all);
     if (threadIdx.x == 0) a.counts[blockIdx.x] = all;
 }
 
@@ -347,8 +410,14 @@ __global__ __launch_bounds__(kTake) void used_kernel(const PageArgs a) {
 // to[page] is that number. *moves is how many there are. The counts of the pages below n that stay.
 __global__ __launch_bounds__(kTake) void compact_kernel(const PageArgs a, int chunks) {
     __shared__ int sums[kTake / 64];
+    __shared__ PageBits<1> pages;
     const int t = threadIdx.x, c = blockIdx.x, first = c * kChunk + t * kEach;
-    const uint32_t used = used_pages(a, first);
+    int4 refs[kEach / 4];
+#pragma unroll
+    for (int k = 0; k < kEach / 4; ++k)
+        refs[k] = four_of(a.old_refs, c * (kChunk / 4) + k * kTake + t, a.pages, 0);
+    const uint32_t used = uint32_t(page_bits<1>(
+        pages, 0, [&](int i) { return in_use(refs[i / kTake]); }));
     int mine, before = 0;
     int rank = scan<kTake>(__popc(used), sums, &mine);
     int n = mine;
@@ -370,17 +439,30 @@ __global__ __launch_bounds__(kTake) void compact_kernel(const PageArgs a, int ch
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int p = first + i;
-        if (p >= a.pages) break;
-        const bool in_use = used >> i & 1;
-        if (p == n) *a.moves = n - rank;
+        const bool u = used >> i & 1;
+        if (p == n && p < a.pages) *a.moves = n - rank;
         if (p < n) {
-            if (!in_use) a.dst[p - rank] = p;
-        } else if (in_use) {
+            if (!u) a.dst[p - rank] = p;
+        } else if (u) {
             a.src[n - 1 - rank] = p;
             a.to[p] = n - 1 - rank;
         }
-        if (p >= n || in_use) a.refs[p] = p < n ? a.old_refs[p] : 0;
-        rank += in_use;
+        rank += u;
+    }
+    // (free pages below n get their counts with their contents; until then any)
+#pragma unroll
+    for (int k = 0; k < kEach / 4; ++k) {
+        const int at = 4 * (c * (kChunk / 4) + k * kTake + t);
+        const int4 x = refs[k];
+        const int y[4] = {at < n ? x.x : 0, at + 1 < n ? x.y : 0, at + 2 < n ? x.z : 0,
+                          at + 3 < n ? x.w : 0};
+        if (at + 4 <= a.pages && (reinterpret_cast<uintptr_t>(a.refs) & 15) == 0) {
+            *reinterpret_cast<int4*>(a.refs + at) = make_int4(y[0], y[1], y[2], y[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + i < a.pages) a.refs[at + i] = y[i];
+        }
     }
 }
 

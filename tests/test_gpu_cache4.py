@@ -69,7 +69,7 @@ def test_codes_of_every_border(gpu, dtype):
                 rows.append(row)
     x = torch.stack(rows)
     # Every power of two that a float32 scale can have and a few at its ends.
-    for power in (0, -3, 100, 124, -121, -124, -130):
+    for power in (0, -3, 100, 124, -121, -124, -127, -128, -129, -130):
         same((x.double() * 2.0 ** power).to(dtype))
 
 
