@@ -20,7 +20,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPer = 16;        // tokens of a workgroup at most
-constexpr int kTablePairs = 1024;  // cosines and sines held
+constexpr int kTablePairs = 1152;  // cosines and sines held
+constexpr int kStill = 8;          // behind a token's pairs: some that do not turn
 
 struct Side {
     const char* src;
@@ -53,7 +54,9 @@ __device__ __forceinline__ T down(float x);
 template <>
 __device__ __forceinline__ float down<float>(float x) { return x; }
 template <>
-__device__ __forceinline__ uint16_t down<uint16_t>(float x) { return uint16_t(f32_to_bf16_bits(x)); }
+__device__ __forceinline__ uint16_t down<uint16_t>(float x) {
+    return __builtin_bit_cast(uint16_t, __bf16(x));
+}
 
 template <typename T, int V>
 struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec {
@@ -118,13 +121,17 @@ __global__ __launch_bounds__(kThreads) void four_append_kernel(const Params p) {
     __shared__ int64_t place[kMaxPer];
     const sparsp_cache& c = p.cache;
     const int t0 = blockIdx.x * p.per.d, count = min(int(p.per.d), p.tokens - t0);
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, row_pairs = p.P + kStill;
     for (int k = threadIdx.x >> 6; k < count; k += kThreads / 64) {
         const int64_t row = place_of(c, p.tokens, t0 + k, lane);
         if (lane == 0) place[k] = row;
     }
-    for (int e = threadIdx.x; e < count * p.P; e += kThreads) {
-        const int k = e / p.P, pr = e % p.P;
+    for (int e = threadIdx.x; p.P > 0 && e < count * row_pairs; e += kThreads) {
+        const int k = e / row_pairs, pr = e % row_pairs;
+        if (pr >= p.P) {
+            turn[e] = make_double2(1.0, 0.0);
+            continue;
+        }
         const int axis = (pr >= p.axis_end[0]) + (pr >= p.axis_end[1]);
         const int64_t at = int64_t(axis) * p.tokens + t0 + k;
         const double x = p.wide ? double(static_cast<const int64_t*>(p.positions)[at])
@@ -148,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void four_append_kernel(const Params p) {
             if (place[k] == kNoSequence) continue;
             const char* in = p.q + int64_t(h) * p.q_head + int64_t(t0 + k) * p.q_token;
             char* out = p.q_out + int64_t(h) * p.out_head + int64_t(t0 + k) * p.out_token;
-            const double2* cs = turn + k * p.P;
+            const double2* cs = turn + k * row_pairs;
             auto put = [&](int ch, const Vec<T, V>& x) {
                 *reinterpret_cast<Vec<T, V>*>(out + ch * int(sizeof(T))) = x;
             };
@@ -187,59 +194,61 @@ __global__ __launch_bounds__(kThreads) void four_append_kernel(const Params p) {
 
     // K and V: units of eight channels; a row's units fill whole groups of four lanes.
     const uint32_t items = uint32_t(count) * c.H * p.units.d;
+    for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
+        const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
+        const uint32_t k = p.heads.quot(row), h = row - k * c.H;
+        const int64_t at = place[k];
+        if (at < 0) continue;
+        const char* kin = p.kv[0].src + int64_t(h) * p.kv[0].head + int64_t(t0 + k) * p.kv[0].token;
+        const char* vin = p.kv[1].src + int64_t(h) * p.kv[1].head + int64_t(t0 + k) * p.kv[1].token;
+        const int ch = int(u) * 8;
+        const Vec<T, 8> x = get<T, 8>(kin, ch), w = get<T, 8>(vin, ch);
+        uint32_t scale[2], codes[2];
+        if (p.P > 0) {
+            const double2* cs = turn + k * row_pairs;
+            double y[8];
+            if (HALF) {
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const Side& sd = p.kv[side];
-        for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
-            const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
-            const uint32_t k = p.heads.quot(row), h = row - k * c.H;
-            const int64_t at = place[k];
-            if (at < 0) continue;
-            const char* in = sd.src + int64_t(h) * sd.head + int64_t(t0 + k) * sd.token;
-            const int ch = int(u) * 8;
-            const Vec<T, 8> x = get<T, 8>(in, ch);
-            uint32_t scale, codes;
-            if (side == 0 && p.P > 0) {
-                const double2* cs = turn + k * p.P;
-                double y[8];
-                if (HALF) {
+                for (int e0 = 0; e0 < 8; e0 += V) {
+                    const int first = ch + e0;
+                    const bool turns = first < 2 * p.P, behind = turns && first >= p.P;
+                    const int far_at = !turns ? first : behind ? first - p.P : first + p.P;
+                    const Vec<T, V> far = get<T, V>(kin, far_at);
+                    const double2* t = cs + (!turns ? p.P : behind ? far_at : first);
+                    const uint32_t flip = behind ? 0u : 0x80000000u;
 #pragma unroll
-                    for (int e0 = 0; e0 < 8; e0 += V) {
-                        const int first = ch + e0, behind = first >= p.P;
-                        const bool turns = first < 2 * p.P;
-                        const Vec<T, V> other =
-                            get<T, V>(in, turns ? behind ? first - p.P : first + p.P : first);
-                        const double2* t = cs + (turns ? first - (behind ? p.P : 0) : 0);
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            const double own = double(up<T>(x.e[e0 + e])), far = double(up<T>(other.e[e]));
-                            const double sn = behind ? t[e].y : -t[e].y;
-                            y[e0 + e] = turns ? own * t[e].x + far * sn : own;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const bool turns = ch + e < 2 * p.P;
-                        const double2 t = cs[turns ? (ch + e) / 2 : 0];
-                        const double x1 = double(up<T>(x.e[e])), x2 = double(up<T>(x.e[e + 1]));
-                        y[e] = turns ? x1 * t.x - x2 * t.y : x1;
-                        y[e + 1] = turns ? x1 * t.y + x2 * t.x : x2;
+                    for (int e = 0; e < V; ++e) {
+                        const float z = __uint_as_float(__float_as_uint(up<T>(far.e[e])) ^ flip);
+                        y[e0 + e] = double(up<T>(x.e[e0 + e])) * t[e].x + double(z) * t[e].y;
                     }
                 }
-                codes = quantise(y, &scale);
             } else {
-                float y[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = up<T>(x.e[e]);
-                codes = quantise(y, &scale);
+                for (int e = 0; e < 8; e += 2) {
+                    const double2 t = cs[min((ch + e) / 2, p.P)];
+                    const double x1 = double(up<T>(x.e[e])), x2 = double(up<T>(x.e[e + 1]));
+                    y[e] = x1 * t.x - x2 * t.y;
+                    y[e + 1] = x1 * t.y + x2 * t.x;
+                }
             }
-            const int64_t to = at + int64_t(h) * c.page;  // (c.page a power of two, heads [page] rows)
-            *reinterpret_cast<uint32_t*>(sd.codes + to * (c.d / 2) + 4 * u) = codes;
-            if (u % 4 == 0) {
-                const int slot = int(to & (c.page - 1));
-                sd.scales[(to - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot] = uint8_t(scale);
-            }
+            codes[0] = quantise(y, scale);
+        } else {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = up<T>(x.e[e]);
+            codes[0] = quantise(y, scale);
+        }
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = up<T>(w.e[e]);
+        codes[1] = quantise(y, scale + 1);
+        const int64_t to = at + int64_t(h) * c.page;  // (c.page a power of two, heads [page] rows)
+        const int slot = int(to & (c.page - 1));
+        const int64_t scale_at = (to - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot;
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            *reinterpret_cast<uint32_t*>(p.kv[side].codes + to * (c.d / 2) + 4 * u) = codes[side];
+            if (u % 4 == 0) p.kv[side].scales[scale_at] = uint8_t(scale[side]);
         }
     }
 }
@@ -256,24 +265,27 @@ __global__ __launch_bounds__(kThreads) void four_read_kernel(const Params p) {
     }
     __syncthreads();
     const uint32_t items = uint32_t(count) * c.H * p.units.d;
+    for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
+        const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
+        const uint32_t k = p.heads.quot(row), h = row - k * c.H;
+        const int64_t at = place[k];
+        if (at == kNoSequence) continue;
+        const int64_t from = max(at, int64_t(0)) + int64_t(h) * c.page;
+        const int slot = int(from & (c.page - 1));
+        const int64_t scale_at = (from - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot;
+        uint32_t codes[2], scale[2];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const Side& sd = p.kv[side];
-        for (uint32_t it = threadIdx.x; it < items; it += kThreads) {
-            const uint32_t row = p.units.quot(it), u = it - row * p.units.d;
-            const uint32_t k = p.heads.quot(row), h = row - k * c.H;
-            const int64_t at = place[k];
-            if (at == kNoSequence) continue;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (at >= 0) {
-                const int64_t from = at + int64_t(h) * c.page;
-                const int slot = int(from & (c.page - 1));
-                const uint32_t codes =
-                    *reinterpret_cast<const uint32_t*>(sd.codes + from * (c.d / 2) + 4 * u);
-                const uint32_t scale =
-                    sd.scales[(from - slot) * (c.d / 32) + int64_t(u / 4) * c.page + slot];
-                x = four_octet(codes, __uint_as_float(scale << 23));
-            }
+        for (int side = 0; side < 2; ++side) {
+            codes[side] = scale[side] = 0;
+            if (at < 0) continue;
+            const Side& sd = p.kv[side];
+            codes[side] = *reinterpret_cast<const uint32_t*>(sd.codes + from * (c.d / 2) + 4 * u);
+            scale[side] = sd.scales[scale_at];
+        }
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const Side& sd = p.kv[side];
+            const uint4 x = four_octet(codes[side], __uint_as_float(scale[side] << 23));
             char* out = const_cast<char*>(sd.src) + int64_t(h) * sd.head + int64_t(t0 + k) * sd.token;
             if constexpr (sizeof(T) == 2) {
                 *reinterpret_cast<uint4*>(out + 16 * u) = x;
@@ -310,7 +322,7 @@ Params params(const FourArgs& f, int pairs) {
     // As in rotate_rows.hip: enough workgroups to fill the GPU four times, then longer runs.
     int per = 1;
     while (per < kMaxPer && a.tokens / (2 * per) >= 1024 &&
-           (pairs == 0 || 2 * per * pairs <= kTablePairs))
+           (pairs == 0 || 2 * per * (pairs + kStill) <= kTablePairs))
         per *= 2;
     p.per = make_div(uint32_t(per));
     return p;
