@@ -86,6 +86,25 @@ class Cache4:
     V: Any
     V_scales: Any
 
+    # Types and shapes are looked at once, when the cache is made, and sizes again in every call.
+    def __post_init__(self):
+        torch, K = _torch(), self.K
+        for name, t in zip(("K", "K_scales", "V", "V_scales"), self.tensors):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch.Tensor")
+            if t.dtype is not torch.uint8 or t.dim() != 4 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous uint8 tensor of four dimensions")
+            if t.device != K.device:
+                raise ValueError(f"{name} is on {t.device}, K on {K.device}")
+        P, H, page, half = K.shape
+        codes, scales = (P, H, page, half), (P, H, half // 16, page)
+        for name, t, shape in (("K_scales", self.K_scales, scales), ("V", self.V, codes),
+                               ("V_scales", self.V_scales, scales)):
+            if t.shape != shape:
+                raise ValueError(f"{name} must have shape {shape} (got {tuple(t.shape)})")
+        # (frozen: set past the dataclass's own refusal)
+        object.__setattr__(self, "_sizes", (P, H, page, 2 * half, K.numel(), self.K_scales.numel()))
+
     @classmethod
     def zeros(cls, pages: int, H: int, page: int, d: int, device="cuda") -> "Cache4":
         """A cache of zeros."""
@@ -103,30 +122,28 @@ class Cache4:
 
     @property
     def d(self) -> int:
-        return self.K.shape[3] * 2
+        return self._sizes[3]
 
 
 def _cache4(cache, page_table, new_off, kv_len):
     """(sparsp_cache4, GPU) of the cache and its sequences."""
-    torch = _torch()
     if not isinstance(cache, Cache4):
         raise TypeError("cache must be a Cache4")
-    if not isinstance(cache.K, torch.Tensor) or cache.K.dim() != 4:
-        raise ValueError("codes must be uint8 [pages, H, page, d / 2]")
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+    if not isinstance(page_table, _torch().Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be an int32 [B, width] tensor")
-    P, H, page, half = cache.K.shape
-    scales = (P, H, half // 16, page)
+    K, Ks, V, Vs = cache.K, cache.K_scales, cache.V, cache.V_scales
+    P, H, page, d, codes, scales = cache._sizes
+    dev = K.get_device()
+    if dev < 0:
+        raise ValueError(f"the cache must be on the GPU (got {K.device})")
+    if K.numel() != codes or V.numel() != codes or Ks.numel() != scales or Vs.numel() != scales:
+        raise ValueError("the cache's tensors have been resized")
     B, width = page_table.shape
-    u8, i32 = torch.uint8, torch.int32
-    k = _on(cache.K, "K codes", None, u8)
-    dev = cache.K.get_device()
+    i32 = _torch().int32
     return _CACHE4.pack(
-        k, _on(cache.K_scales, "K scales", dev, u8, scales),
-        _on(cache.V, "V codes", dev, u8, cache.K.shape),
-        _on(cache.V_scales, "V scales", dev, u8, scales), _on(page_table, "page_table", dev, i32),
-        _on(new_off, "new_off", dev, i32, (B + 1,)), _on(kv_len, "kv_len", dev, i32, (B,)),
-        P, H, page, 2 * half, width, B, 0, 0), dev
+        K.data_ptr(), Ks.data_ptr(), V.data_ptr(), Vs.data_ptr(),
+        _on(page_table, "page_table", dev, i32), _on(new_off, "new_off", dev, i32, (B + 1,)),
+        _on(kv_len, "kv_len", dev, i32, (B,)), P, H, page, d, width, B, 0, 0), dev
 
 
 def sparsp_paged_append4(K, V, cache: Cache4, page_table, new_off, kv_len,

@@ -89,7 +89,7 @@ __device__ __forceinline__ void copy_rows(const u32x4_t& desc, const int (&off)[
 // D: channels of a row in LDS; those from C on are zero and left out of the products (d = 96,
 // 32 heads, 675 tokens over 24,153: 283 us, with all 128 328 us).
 template <int D, int C, bool WINDOW, bool FOUR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
 void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     constexpr int TILE = kKeys * D;
     constexpr int NCH = D / 8;         // 16-byte chunks of a row
