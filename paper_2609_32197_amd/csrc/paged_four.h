@@ -337,11 +337,18 @@ struct FourStage {
             const bool is_k = SIDES == 2 ? n == 0 : side == 0;
             const float s = __uint_as_float(scale[n] << 23);
             uint16_t* row = (is_k ? k : v) + key * D;
-            const int swizzle = is_k ? ks : vs;
+            // Eight lanes write 16 bytes each to all 32 banks: lanes whose chunks the swizzle does not
+            // keep apart take theirs in another order (attend4-chunks of perf/more_operators.py 659 us
+            // in the same one, 8 cycles more a store, and 650 so; at d = 64, where a lane's side
+            // decides as well, the choice costs more: 369 and 400 us).
+            const int turn = D == 128 && (group & 2) ? (is_k ? 2 : 1) : 0;
+            const int swizzle = (is_k ? ks : vs) ^ turn;
             const uint32_t w[4] = {codes[n].x, codes[n].y, codes[n].z, codes[n].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<uint4*>(row + ((4 * group + j) ^ swizzle) * 8) = four_octet(w[j], s);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = turn == 2 ? w[j ^ 2] : turn == 1 ? w[j ^ 1] : w[j];
+                *reinterpret_cast<uint4*>(row + ((4 * group + j) ^ swizzle) * 8) = four_octet(c, s);
+            }
         }
     }
 };

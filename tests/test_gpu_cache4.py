@@ -381,3 +381,41 @@ def test_run_beside_the_cache_of_rows(gpu):
         top = float(v.abs().max())
         assert (a.double() - b.double()).abs().max() <= 4 * 2.0 ** -8 * top
         assert (la - lb).abs().max() <= 2.0 ** -17
+
+
+@pytest.mark.parametrize("dtype,new", [(BF, (1, 2)), (BF, (70, 9)), (F, (1, 30))])
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 24])
+@pytest.mark.parametrize("seen", [dict(), dict(window=120, sinks=9)])
+def test_scores_of_2_to_the_24(gpu, dtype, new, size, seen):
+    """Scores size + 0, 2, 4 or 6, every one of them a float32: their differences count, whatever is
+    subtracted from them on the way. (A product of each is exact, so e of the tolerance is the
+    2^-22 of the largest difference, 6, that c2 and its product are off by.)"""
+    kv = (300, 700)
+    bt = B.Batch4(59, dtype, 4, 2, 32, 16, new, kv)
+    x = torch.zeros(bt.K.shape, dtype=torch.float64)
+    x[..., 0] = 1.0
+    x[..., 1] = 2.0 * torch.randint(0, 4, bt.K.shape[:3], generator=bt.g)
+    x[..., 2] = 6.0  # (the scale is one)
+    live = ~torch.isnan(bt.K[..., 0])
+    codes, scales = B.quantise(x)
+    assert torch.equal(B.values(codes, scales), x)
+    scales[~live] = 255
+    bt.four[:2] = [codes, scales.transpose(-1, -2).contiguous()]
+    bt.K.copy_(torch.where(live[..., None], x, float("nan")))
+    bt.Q.zero_()
+    bt.Q[..., 0], bt.Q[..., 1] = size, 1.0
+    O, lse = run(bt, softmax_scale=1.0, **seen)
+    wO, wL, _, _ = B.attention(bt, scale=1.0, **seen)
+    A = B.attention(bt_abs(bt), scale=1.0, **seen)[0]
+    N, half = max(kv), R.HALF[dtype]
+    r = 2.0 ** -8 if dtype is BF else 0.0
+    tol = A * (r + 4 * 6 * 2.0 ** -22 + 2 * (3 * N + 64) * B.U + 2.0 ** -18) + half * wO.abs()
+    R.close(O, wO, tol, "O")
+    R.close(lse, wL, 4 * B.U * wL.abs() + 2.0 ** -16, "lse")
+
+
+def bt_abs(bt):
+    import copy
+    other = copy.copy(bt)
+    other.V = bt.V.abs()
+    return other
