@@ -2,6 +2,8 @@
 
 import os
 import re
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -28,6 +30,28 @@ def rows(at=3 * AT, heads=4, tokens=5, d=64):
 def status(rc):
     assert rc < 0, "not refused"
     return sp.STATUS[rc], sp.load_library().sparsp_last_error().decode()
+
+
+def test_abi_under_asan_and_ubsan(tmp_path):
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    cxx = os.environ.get("CXX") or shutil.which("g++")
+    if not cxx or not os.path.exists(os.path.join(rocm, "include", "hip", "hip_runtime_api.h")):
+        pytest.skip("needs g++ and the HIP runtime API headers")
+    exe = str(tmp_path / "bounded_host_check")
+    csrc = os.path.join(ROOT, "paper_2609_32197_amd", "csrc")
+    srcs = [os.path.join(csrc, f) for f in ("api.cpp", "api_cache.cpp", "api_bounded.cpp",
+                                            "host_plan.cpp")]
+    srcs += [os.path.join(ROOT, "tests", "hostcheck", f)
+             for f in ("stub_launchers.cpp", "cache_stub_launchers.cpp", "bounded_stub_launchers.cpp",
+                       "bounded_host_check.cpp")]
+    r = subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer",
+                        "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                        "-D__HIP_PLATFORM_AMD__", f"-I{os.path.join(rocm, 'include')}", *srcs, "-o",
+                        exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
+    assert " 0 failures" in r.stdout
 
 
 def test_library_exports_every_declared_symbol():
