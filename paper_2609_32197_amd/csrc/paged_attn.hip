@@ -360,6 +360,51 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a, con
     }
 }
 
+// Joins the parts of a tail's rows: a workgroup eight rows of a tile, 32 lanes a row.
+template <bool WINDOW>
+__global__ __launch_bounds__(256) void paged_tail_kernel(const PagedArgs a, const PagedPlan plan) {
+    const sparsp_cache& c = a.cache;
+    const int G = a.q_heads / c.H, q = blockIdx.x >> 4;
+    const int at = plan.tail + (q >> 3), unit = at / plan.tiles * 8 + (q & 7);
+    if (unit >= c.B * c.H) return;
+    const int b = unit / c.H, hk = unit % c.H;
+    const Seq s = sequence(c, a.tokens, b);
+    const int rows = s.n * G, tiles = (rows + plan.rows - 1) / plan.rows;
+    const int tile = tiles - 1 - at % plan.tiles;  // (the last ones come first)
+    if (tile < 0) return;
+    int len = s.kv;
+    if constexpr (WINDOW)
+        len = span_of(a, s, G, tile * plan.rows, min(rows, (tile + 1) * plan.rows) - 1, plan.grain).len;
+    const int keys = part_keys(plan, len);
+    if (len <= keys) return;
+    const int parts = (len + keys - 1) / keys;
+    const int mine = (blockIdx.x & 15) * 8 + (threadIdx.x >> 5), ch = (threadIdx.x & 31) * 4;
+    const int r = tile * plan.rows + mine;
+    if (r >= rows || ch >= c.d) return;
+    const int64_t from = (int64_t(q) * plan.rows + mine) * plan.parts;
+    const float c2 = a.scale * kLog2e;
+    float top = -INFINITY;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, plan.part_ref[from + p]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float x[4] = {}, total = 0.f;
+    for (int p = 0; p < parts; ++p) {
+        const float w = plan.part_sum[from + p] *
+                        __builtin_amdgcn_exp2f((plan.part_ref[from + p] - base) * c2);
+        const floatx4 y = *reinterpret_cast<const floatx4*>(plan.part_o + (from + p) * c.d + ch);
+        total += w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += w * y[e];
+    }
+    const bool any = total > 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = any ? x[e] / total : 0.f;
+    const int i = r / G, h = hk * G + r % G;
+    store4(a.O, int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token + ch, a.out_bf16, x);
+    if (ch == 0 && a.lse)
+        a.lse[int64_t(h) * a.tokens + s.q0 + i] =
+            any ? fmaf(top, a.scale, __logf(total)) : -INFINITY;
+}
+
 // The launch for what is known of the lengths. bf16 rows of more than 16 a sequence go to
 // the kernel of 128-row tiles (d = 128: 32 sequences of 8,000, 32 rows each: 237 us 32 rows at
 // a time from registers, 198 us; one of 2,000 with 24 rows 13.0 and 15.3 us). At d <= 64, where
@@ -457,6 +502,33 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     // (in whole units of d + 1 numbers for every row)
     const int64_t unit = all_rows * (c.d + 1) * 4;
     r.bytes = parts > 1 ? (parts * part_bytes + unit - 1) / unit * unit : 0;
+    // Whole row tiles of 128 in more than one round of two a CU (three at d <= 64), that is 64 an XCD:
+    // those of the last round are cut into as many parts as fill it best, for the partial rows of that
+    // round alone (4 bits, 8 key heads, 1,021 and 1,500 tokens over up to 16,384: 85 tiles an XCD, 659
+    // us whole, 558 us with the last 21 in parts).
+    if ((a.window || a.k_scales) && r.rows == 128 && parts == 1 && !r.plan.flat && pairs % 8 == 0 &&
+        tiles == (rows + r.rows - 1) / r.rows) {
+        const int64_t slots = (c.d <= 64 ? 3 : 2) * kCus / 8;
+        // (of each sequence's last tile half counts: what `flat` has too many is half of them)
+        const int64_t mine = std::min(c.H * (flat - c.B / 2), pairs * tiles) / 8;
+        const int64_t tail = (mine - 1) / slots * slots, last = mine - tail;
+        const int64_t all = pairs / 8 * tiles - tail;
+        double least = 1.0;
+        int64_t cut = 1;
+        for (int64_t p = 2; tail > 0 && p <= std::min<int64_t>(8, rounds / 8); ++p) {
+            const double time = double((last * p + slots - 1) / slots) / p + 0.03 * p;
+            if (time < least && all * 8 * r.rows * p * (c.d + 2) * 4 <= ws_bytes) {
+                least = time;
+                cut = p;
+            }
+        }
+        if (cut > 1) {
+            r.plan.tail = int(tail);
+            r.plan.parts = int(cut);
+            r.plan.step = 8 * round;  // (even parts for every length)
+            r.bytes = all * 8 * r.rows * cut * (c.d + 2) * 4;
+        }
+    }
     return r;
 }
 
@@ -492,13 +564,19 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
     Shape r = shape(a, a.ws ? a.ws_bytes : 0);
     if (r.plan.parts > 1) {
         r.plan.part_o = static_cast<float*>(a.ws);
-        const int64_t rows = int64_t(a.q_heads) * a.tokens * r.plan.parts;
+        const int64_t rows = (r.plan.tail ? int64_t(tail_tiles(r.plan, a.cache)) * r.rows
+                                          : int64_t(a.q_heads) * a.tokens) * r.plan.parts;
         r.plan.part_sum = r.plan.part_o + rows * a.cache.d;
         r.plan.part_ref = r.plan.part_sum + rows;
     }
     const hipError_t e = r.rows == 128 ? launch_paged_tiles(a, r.plan, s) : launch_few(a, r, s);
     if (e != hipSuccess || r.plan.parts == 1) return e;
     const int most_new = a.max_new > 0 && a.max_new < a.tokens ? a.max_new : a.tokens;
+    if (r.plan.tail) {
+        const auto join = a.window ? paged_tail_kernel<true> : paged_tail_kernel<false>;
+        join<<<tail_tiles(r.plan, a.cache) * (r.rows / 8), 256, 0, s>>>(a, r.plan);
+        return hipGetLastError();
+    }
     const int64_t pairs = int64_t(a.cache.B) * a.q_heads;
     const bool shared = pairs * most_new <= 16 * kCus;
     const int64_t runs = shared ? most_new : (most_new + 7) / 8;  // workgroups of a head

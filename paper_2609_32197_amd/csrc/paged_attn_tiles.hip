@@ -109,8 +109,13 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
+    // (bf16 rows without a window have no tail)
+    const int tail = __builtin_amdgcn_readfirstlane(work.tail);
+    auto keys_of = [&](int len) {
+        return (WINDOW || FOUR) && plan.tail && tail < 0 ? max(len, 1) : part_keys(plan, len);
+    };
     Span span = {0, 0, s.kv, 0};
-    int keys = part_keys(plan, s.kv);
+    int keys = keys_of(s.kv);
     bool whole = s.kv <= keys;
     if (!WINDOW && part > 0 && part * int64_t(keys) >= s.kv) return;
     int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
@@ -152,7 +157,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
         const int tile = n_tiles - 1 - turns;
         if constexpr (WINDOW) {
             span = span_of(a, s, G, tile * kRowsTile, min(rows, (tile + 1) * kRowsTile) - 1, kKeys);
-            keys = part_keys(plan, span.len);
+            keys = keys_of(span.len);
             whole = span.len <= keys;
             if (part > 0 && part * int64_t(keys) >= span.len) continue;
             lo = part * keys;
@@ -445,7 +450,9 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
             const bool any = total > 0.f;
             const float inv = any ? 1.f / total : 0.f;
             const bool far = lim[n] == kFar;
-            const int64_t at = int64_t(h) * a.tokens + s.q0 + i;
+            int64_t at = int64_t(h) * a.tokens + s.q0 + i;
+            if ((WINDOW || FOUR) && !whole && plan.tail)
+                at = int64_t(tail) * kRowsTile + wave * 32 + n * 16 + col;
             const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
                                      : (at * plan.parts + part) * c.d;
 #pragma unroll
@@ -467,7 +474,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                     const float f = far ? 1.f : __builtin_amdgcn_exp2f(fmaf(-ref, c2, -base[n]));
                     plan.part_sum[at * plan.parts + part] = any ? total * f : 0.f;
                     plan.part_ref[at * plan.parts + part] = any ? ref : -INFINITY;
-                } else if (a.lse) {
+                } else if (a.lse) {  // (at: of a whole row)
                     a.lse[at] = !any  ? -INFINITY
                                 : far ? fmaf(base[n], a.scale, __logf(total))
                                       : (__log2f(total) - base[n]) * kLn2;

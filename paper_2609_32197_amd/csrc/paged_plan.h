@@ -11,6 +11,10 @@ namespace sparsp {
 struct PagedPlan {
     int tiles, parts, step, flat;
     int rows, grain;  // rows of a tile; with a window, what its bounds are rounded to
+    // With `tail` the workgroups of an XCD from that number on, and they alone, walk one of `parts` parts
+    // of their keys each: the last round of row tiles, which would leave slots empty. Their partial
+    // rows lie by row of the tile, tiles in the order of their workgroups.
+    int tail;
     float* part_o;  // [q_heads, tokens, parts, d], normalised
     // A part's sum of exponentials [q_heads, tokens, parts], and behind all of them the score, not
     // yet scaled, that they are relative to (-inf: the part has nothing). Not the log of one times
@@ -66,6 +70,7 @@ __device__ __forceinline__ Unit unit_of(int u, int pairs) {
 // part of the keys.
 struct Work {
     int b, hk, part, tile, stride;
+    int tail;  // number of a tail's tile, or -1
 };
 // Row tile number f of all sequences' tiles of ROWS rows. Each wave counts the tiles of 64
 // sequences at a time.
@@ -101,6 +106,15 @@ template <int ROWS>
 __device__ __forceinline__ bool work_of(const PagedPlan& p, const sparsp_cache& c, int tokens, int G,
                                         Work* w) {
     const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
+    w->tail = -1;
+    if (p.tail) {
+        const int behind = k - p.tail, at = behind < 0 ? k : p.tail + behind / p.parts;
+        const int unit = at / p.tiles * 8 + xcd;
+        if (unit >= c.B * c.H) return false;
+        *w = {unit / c.H, unit % c.H, behind < 0 ? 0 : behind % p.parts, at % p.tiles, p.tiles,
+              behind < 0 ? -1 : (at - p.tail) * 8 + xcd};
+        return true;
+    }
     if (p.flat) {
         const int turn = (k >> 3) * 8 + xcd, units = c.H * p.parts;
         const int run = turn / units, f = run * 8 + (k & 7);
@@ -113,10 +127,15 @@ __device__ __forceinline__ bool work_of(const PagedPlan& p, const sparsp_cache& 
     const int unit = k / p.tiles * 8 + xcd;
     if (unit >= c.B * c.H * p.parts) return false;
     const auto [bh, part] = unit_of(unit, c.B * c.H);
-    *w = {bh / c.H, bh % c.H, part, k % p.tiles, p.tiles};
+    *w = {bh / c.H, bh % c.H, part, k % p.tiles, p.tiles, -1};
     return true;
 }
+// Tiles of the tail.
+inline int tail_tiles(const PagedPlan& p, const sparsp_cache& c) {
+    return p.tail ? ((c.B * c.H + 7) / 8 * p.tiles - p.tail) * 8 : 0;
+}
 inline int workgroups(const PagedPlan& p, const sparsp_cache& c) {
+    if (p.tail) return p.tail * 8 + tail_tiles(p, c) * p.parts;
     return p.flat ? ((p.flat + 7) / 8 * c.H * p.parts + 7) / 8 * 64
                   : (c.B * c.H * p.parts + 7) / 8 * 8 * p.tiles;
 }

@@ -419,3 +419,44 @@ def bt_abs(bt):
     other = copy.copy(bt)
     other.V = bt.V.abs()
     return other
+
+
+
+@pytest.mark.parametrize("d,Hq,new,kv", [(128, 8, (1100,), (4000,)),           # nine tiles of eight heads
+                                         (96, 64, (1030,), (2100,)),           # 65 a head: one over a round
+                                         (64, 96, (900, 500), (3000, 2200)),   # three a CU
+                                         (128, 64, (700, 500), (1300, 2900))])
+@pytest.mark.parametrize("seen", [dict(), dict(causal=False), dict(window=2500, sinks=40)])
+def test_last_round_in_parts(gpu, d, Hq, new, kv, seen):
+    """Row tiles of a little over a round of workgroups: with every workspace, against eight heads of
+    their own, which are one round, and the same twice."""
+    H = 8
+    bt = B.Batch4(60, BF, Hq, H, d, 64, new, kv)
+    cache, t, q = bt.to4("cuda")
+    w = {k: seen[k] for k in seen if k != "causal"}
+    hints = dict(max_new=max(new), max_kv=max(kv))
+    full = sp.sparsp_paged_attn4_workspace_bytes(cache, t["page_table"], bt.T, Hq, **hints, **w)
+    G = Hq // H
+    assert full > 0
+    want, lse = zip(*(sp.sparsp_paged_attn4(q[g::G].contiguous(), cache, **t, out_dtype=sp.F32, **seen)
+                      for g in range(G)))
+    for nbytes in (0, full // 2, full):
+        ws = torch.full((nbytes + 256,), 255, dtype=torch.uint8, device="cuda")
+        O, L = sp.sparsp_paged_attn4(q, cache, **t, **hints, workspace=ws[:nbytes], out_dtype=sp.F32,
+                                     **seen)
+        again = sp.sparsp_paged_attn4(q, cache, **t, **hints, workspace=ws[:nbytes], out_dtype=sp.F32,
+                                      **seen)
+        assert torch.equal(O, again[0]) and torch.equal(L, again[1])
+        assert (ws[nbytes:] == 255).all()
+        for g in range(G):
+            # Both round probabilities to bf16, by 2^-8 of sums of p |v| below max |v|.
+            assert (O[g::G] - want[g]).abs().max() <= 2 * 2.0 ** -8 * 6
+            assert (L[g::G] - lse[g]).abs().max() <= 2.0 ** -16
+    # Some heads against 64 bits.
+    some = B.Batch4(60, BF, Hq, H, d, 64, new, kv)
+    assert torch.equal(some.Q, bt.Q)
+    some.Hq, some.H, some.Q = 1, 1, bt.Q[G - 1:G]
+    some.K, some.V = bt.K[:, :1], bt.V[:, :1]
+    wO, wL, tO, tL = B.attention(some, terms=3, out_dtype=F, **seen)
+    R.close(O[G - 1:G], wO, tO, "O")
+    R.close(L[G - 1:G], wL, tL, "lse")
