@@ -109,15 +109,12 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const int b = work.b, hk = work.hk, part = work.part;
     const Seq s = sequence(c, a.tokens, b);
     const int rows = s.n * G;
-    // (bf16 rows without a window have no tail)
-    const int tail = __builtin_amdgcn_readfirstlane(work.tail);
-    auto keys_of = [&](int len) {
-        return (WINDOW || FOUR) && plan.tail && tail < 0 ? max(len, 1) : part_keys(plan, len);
-    };
+    // Calls with a window or over 4 bits can have a tail, and find their part for each tile.
+    constexpr bool EACH = WINDOW || FOUR;
     Span span = {0, 0, s.kv, 0};
-    int keys = keys_of(s.kv);
+    int keys = part_keys(plan, s.kv);
     bool whole = s.kv <= keys;
-    if (!WINDOW && part > 0 && part * int64_t(keys) >= s.kv) return;
+    if (!EACH && part > 0 && part * int64_t(keys) >= s.kv) return;
     int lo = part * keys, part_end = min(s.kv - lo, keys) + lo;
     const float c2 = a.scale * kLog2e;
     const int shift = __builtin_ctz(c.page);
@@ -155,9 +152,12 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     for (int turns = work.tile; turns * int64_t(kRowsTile) < rows; turns += work.stride) {
         const int n_tiles = (rows + kRowsTile - 1) / kRowsTile;
         const int tile = n_tiles - 1 - turns;
-        if constexpr (WINDOW) {
-            span = span_of(a, s, G, tile * kRowsTile, min(rows, (tile + 1) * kRowsTile) - 1, kKeys);
-            keys = keys_of(span.len);
+        if constexpr (EACH) {
+            if constexpr (WINDOW)
+                span = span_of(a, s, G, tile * kRowsTile, min(rows, (tile + 1) * kRowsTile) - 1, kKeys);
+            // (of a workgroup's tiles, which are more where max_new was too small, the first is the tail's)
+            const bool all = plan.tail && (work.tail < 0 || turns != work.tile);
+            keys = all ? max(span.len, 1) : part_keys(plan, span.len);
             whole = span.len <= keys;
             if (part > 0 && part * int64_t(keys) >= span.len) continue;
             lo = part * keys;
@@ -451,8 +451,8 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
             const float inv = any ? 1.f / total : 0.f;
             const bool far = lim[n] == kFar;
             int64_t at = int64_t(h) * a.tokens + s.q0 + i;
-            if ((WINDOW || FOUR) && !whole && plan.tail)
-                at = int64_t(tail) * kRowsTile + wave * 32 + n * 16 + col;
+            if (EACH && !whole && plan.tail)
+                at = int64_t(work.tail) * kRowsTile + wave * 32 + n * 16 + col;
             const int64_t to = whole ? int64_t(h) * a.o_head + int64_t(s.q0 + i) * a.o_token
                                      : (at * plan.parts + part) * c.d;
 #pragma unroll

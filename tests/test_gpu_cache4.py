@@ -448,6 +448,11 @@ def test_last_round_in_parts(gpu, d, Hq, new, kv, seen):
                                       **seen)
         assert torch.equal(O, again[0]) and torch.equal(L, again[1])
         assert (ws[nbytes:] == 255).all()
+        # A max_new below the truth sizes the launch for fewer row tiles than there are.
+        few = sp.sparsp_paged_attn4(q, cache, **t, max_new=max(new) - 200, max_kv=max(kv) // 2,
+                                    workspace=ws[:nbytes], out_dtype=sp.F32, **seen)
+        assert (few[0] - O).abs().max() <= 2 * 2.0 ** -8 * 6
+        assert (few[1] - L).abs().max() <= 2.0 ** -16
         for g in range(G):
             # Both round probabilities to bf16, by 2^-8 of sums of p |v| below max |v|.
             assert (O[g::G] - want[g]).abs().max() <= 2 * 2.0 ** -8 * 6
