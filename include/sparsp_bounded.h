@@ -29,7 +29,8 @@ extern "C" {
  * sees the cached tokens t <= p with t > p - window (itself and the window - 1 before it) or
  * t < sinks. Table entries of pages that no row sees are not read, so they may name no page or
  * another sequence's; where a page is seen in part, all its tokens must be finite. window >= 1,
- * sinks >= 0. A launch costs what the window holds, not what the cache does.
+ * sinks >= 0. A launch costs what the window holds, not what the cache does. (Its lse is not one for
+ * sparsp_paged_weights, whose rows see every cached token.)
  */
 int sparsp_paged_attn_window(const sparsp_cache* cache, int32_t tokens, const sparsp_rows* Q,
                              const sparsp_rows* O, int32_t out_dtype, float* lse, int32_t window,

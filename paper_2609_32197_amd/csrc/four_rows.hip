@@ -11,7 +11,11 @@
 // is rotated in float32 as by sparsp_rope.
 //
 // A thread takes eight channels, a dword of codes; four neighbours share a scale. A workgroup takes
-// `per` tokens and shares their cosines and sines over all heads, as in rotate_rows.hip.
+// `per` tokens and shares their cosines and sines over all heads, as in rotate_rows.hip. Prompts of
+// 8,400 tokens, 20 heads of Q, K and V of 128, half of each rotated: 56 us, 3.4 TB/s, the vector unit
+// busy with the 64-bit rotation and 20 instructions a code (with codes by comparisons in 64 bits
+// instead of the conversion instruction 77 us); the same read back 25 us, 4.4 TB/s. With 2 or 4
+// tokens a workgroup both take 79 us, with one 88, with eight 85.
 #include "cache_device.h"
 #include "paged_four.h"
 

@@ -7,7 +7,10 @@
 // d = 128), so what bounds it is their issue as much as reading: everything else in the loop is kept
 // from the vector unit. A tile's page is the same for all lanes, so its address is scalar, and lanes
 // add constants. The reference of a row's exponentials moves only where they grow past it, as in
-// paged_attn_tiles.hip, so a tile takes no maximum and rescales nothing.
+// paged_attn_tiles.hip, so a tile takes no maximum and rescales nothing. 64 sequences of 400 to 9,001
+// tokens, 8 key heads, one new token each: 46 us (184 MB, 4.0 TB/s; of 9,000 each 5.0 TB/s, 192 of
+// them 5.65), 59 us as one more tile type of paged_rows_kernel. One tile in flight and four waves a
+// SIMD spill (64 of 9,000: 172 us), two waves and three tiles gain nothing (126.8 and 126.8 us).
 #include "paged_four.h"
 
 namespace sparsp {

@@ -356,7 +356,8 @@ def sparsp_paged_attn(Q, K_cache, V_cache, page_table, new_off, kv_len, causal: 
     long caches are split among workgroups; without, one workgroup walks a sequence's keys.
 
     window: a token sees itself and the window - 1 tokens before it, and the sequence's first
-    `sinks` ones. Pages that no row sees are not read; their table entries may name no page.
+    `sinks` ones. Pages that no row sees are not read; their table entries may name no page. The lse
+    is then not one for sparsp_paged_weights, whose rows see the whole cache.
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, None, page_table, new_off, kv_len)
