@@ -468,7 +468,11 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     const int64_t flat = a.tokens * int64_t(G) / r.rows + c.B;
     const int64_t live = std::min(pairs * tiles, c.H * flat);
     int64_t parts = std::min(rounds, int64_t(std::sqrt(10.0 * double(rounds))));
-    if (rounds <= 3 + (r.rows == 128 ? std::min<int64_t>(4, live * parts / 128) : 0)) parts = 1;
+    // With a window and over 4 bits few rows stay whole for six rounds, at which the second kernel and
+    // its launch cost more than a shorter walk saves (3 sequences, 2 key heads; 4 bits, 613 tokens
+    // 9.6 us in 5 parts, 8.1 us whole, and 1,000 9.5 us either way; 400 of bf16 9.9 and 8.4 us).
+    const int brief = r.rows < 128 && (a.window || a.k_scales) ? 6 : 3;
+    if (rounds <= brief + (r.rows == 128 ? std::min<int64_t>(4, live * parts / 128) : 0)) parts = 1;
     if (live * parts > 2 * kCus) {
         int64_t fill = 2 * kCus / std::min<int64_t>(live, 2 * kCus);
         if (rounds >= 16 && live < 2 * kCus && live * fill < 3 * kCus / 2) fill *= 4;
