@@ -281,10 +281,10 @@ def _buffers(caches, pages, dev):
     packed, count = b"", 0
     for c in caches:
         for t in c.tensors if isinstance(c, Cache4) else (c,):
-            at = _on(t, "a cache", dev)
-            if t.dim() < 2 or t.shape[0] != pages:
-                raise ValueError(f"a cache must be [pages = {pages}, ...] (got {tuple(t.shape)})")
-            packed += _BUFFER.pack(at, t.numel() // pages * t.element_size())
+            at, shape = _on(t, "a cache", dev), t.shape
+            if len(shape) < 2 or shape[0] != pages:
+                raise ValueError(f"a cache must be [pages = {pages}, ...] (got {tuple(shape)})")
+            packed += _BUFFER.pack(at, t.nbytes // pages)
             count += 1
     return packed or None, count
 
@@ -292,9 +292,10 @@ def _buffers(caches, pages, dev):
 def _page_workspace(packed, rows, workspace, like, dev, stream):
     """Address and bytes of a page call's workspace, and the tensor that holds it."""
     if workspace is None:
-        nbytes = int(load_library().sparsp_pages_workspace_bytes(packed, rows))
+        nbytes = load_library().sparsp_pages_workspace_bytes(packed, rows)
         _check(nbytes if nbytes < 0 else 0)
         workspace = _new(like, (nbytes,), _torch().uint8, stream)
+        return workspace.data_ptr(), nbytes, workspace
     return _on(workspace, "workspace", dev), workspace.numel() * workspace.element_size(), workspace
 
 
@@ -303,6 +304,7 @@ def _out(t, name, like, shape, dev, stream):
     i32 = _torch().int32
     if t is None:
         t = _new(like, shape, i32, stream)
+        return t, t.data_ptr()
     return t, _on(t, name, dev, i32, shape)
 
 
