@@ -125,7 +125,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
     const uint64_t k_base = (reinterpret_cast<uint64_t>(c.K) & 0xffffffffffffull) + head_at;
     const uint64_t v_base = (reinterpret_cast<uint64_t>(c.V) & 0xffffffffffffull) + head_at;
     [[maybe_unused]] FourStage<D> stage;
-    if constexpr (FOUR) stage.init(tid);
+    if constexpr (FOUR) stage.init(c, hk, tid);
     const uint32_t k_lds = __builtin_amdgcn_readfirstlane(
         uint32_t(reinterpret_cast<uintptr_t>(&lds[0][0][16 * wave * D])));
 
@@ -262,7 +262,7 @@ void paged_tiles_kernel(const PagedArgs a, const PagedPlan plan) {
                 const int key = t0 + stage.key;
                 const int token = WINDOW ? span.cached(key) : key;
                 const int p = page_list[(key >> list_shift) - p0];
-                stage.load(a, token < s.kv ? p : -1, hk, token);
+                stage.load(a, token < s.kv ? p : -1, token);
             };
             auto put = [&](auto buf_c) {
                 constexpr int buf = decltype(buf_c)::value;

@@ -33,11 +33,6 @@ __device__ __forceinline__ uint4 four_octet(uint32_t w, float scale) {
                       four_pair<3>(w, scale));
 }
 
-// First row of head hk on `page` (-1: page 0, whose values the callers mask).
-__device__ __forceinline__ int64_t four_head(const sparsp_cache& c, int page, int hk) {
-    return int64_t(page < 0 ? 0 : page) * c.H + hk;
-}
-
 // Rows of Q in float32 (TERMS 3) enter the products as three bf16 each, which hold them whole, and so
 // do probabilities; rows in bf16 (TERMS 1) as they are, and probabilities as two. C: channels.
 template <int TERMS, int C>
@@ -305,20 +300,28 @@ struct FourStage {
     uint4 codes[SIDES];
     uint32_t scale[SIDES];
     int key, group, side;
+    uint32_t page_codes, page_scales;  // bytes of a page
+    uint32_t code_at, scale_at;        // this thread's in the first row of page 0
+    bool there;
 
-    __device__ __forceinline__ void init(int tid) {
+    __device__ __forceinline__ void init(const sparsp_cache& c, int hk, int tid) {
         side = D == 128 ? 0 : tid >> 7;
         group = tid % GROUPS;
         key = tid / GROUPS % 64;
+        there = 32 * group < c.d;
+        const uint32_t g = there ? group : 0, groups = uint32_t(c.d) / 32;
+        page_codes = uint32_t(c.H * c.page * (c.d / 2));
+        page_scales = uint32_t(c.H * c.page) * groups;
+        code_at = uint32_t(hk * c.page) * uint32_t(c.d / 2) + 16 * g;
+        scale_at = (uint32_t(hk) * groups + g) * c.page;
     }
     // token: the tile's cached token of this thread's key, on `page` (-1: none).
-    __device__ __forceinline__ void load(const PagedArgs& a, int page, int hk, int token) {
+    __device__ __forceinline__ void load(const PagedArgs& a, int page, int token) {
         const sparsp_cache& c = a.cache;
-        const bool live = page >= 0 && 32 * group < c.d;
-        const int64_t head = four_head(c, page, hk);
-        const int row = token & (c.page - 1), g = 32 * group < c.d ? group : 0;
-        const int64_t at = ((head * c.page + row) * c.d + 32 * g) / 2;
-        const int64_t scale_at = (head * (c.d >> 5) + g) * c.page + row;
+        const bool live = page >= 0 && there;
+        const uint32_t row = token & (c.page - 1), p = max(page, 0);
+        const uint64_t at = uint64_t(p) * page_codes + (code_at + row * uint32_t(c.d / 2));
+        const uint64_t scales = uint64_t(p) * page_scales + (scale_at + row);
 #pragma unroll
         for (int n = 0; n < SIDES; ++n) {
             const bool k = SIDES == 2 ? n == 0 : side == 0;
@@ -326,7 +329,7 @@ struct FourStage {
             scale[n] = 0;
             if (live) {
                 codes[n] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(k ? c.K : c.V) + at);
-                scale[n] = (k ? a.k_scales : a.v_scales)[scale_at];
+                scale[n] = (k ? a.k_scales : a.v_scales)[scales];
             }
         }
     }
