@@ -3,7 +3,7 @@
 // With a the largest magnitude of 32 channels the scale is 2^e, e = floor(log2 a) - 2, so that every
 // magnitude is below 8 of it; a code is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even one,
 // 6 for what is larger. All that is exact: e comes from the exponents' bits alone, and a magnitude is
-// rounded once, by rint of a multiple of a power of two.
+// rounded once, by the conversion instruction.
 //
 // K is rotated on the way in 64 bits. A code jumps by a third of its value where a value crosses a
 // border, so that with 32 bits it would depend, once in some 10^6 values, on the rounding of a
@@ -13,8 +13,8 @@
 // A thread takes eight channels, a dword of codes; four neighbours share a scale. A workgroup takes
 // `per` tokens and shares their cosines and sines over all heads, as in rotate_rows.hip. Prompts of
 // 8,400 tokens, 20 heads of Q, K and V of 128, half of each rotated: 56 us, 3.4 TB/s, the vector unit
-// busy with the 64-bit rotation and 20 instructions a code (with codes by comparisons in 64 bits
-// instead of the conversion instruction 77 us); the same read back 25 us, 4.4 TB/s. With 2 or 4
+// busy with the 64-bit rotation (with codes by comparisons in 64 bits instead of the conversion
+// instruction 77 us); the same read back 25 us, 4.4 TB/s. With 2 or 4
 // tokens a workgroup both take 79 us, with one 88, with eight 85.
 #include "cache_device.h"
 #include "paged_four.h"
@@ -101,11 +101,15 @@ __device__ __forceinline__ uint32_t quantise(const float (&y)[8], uint32_t* scal
 // A float64 over 2^e is cut to float32, with the last bit set if that leaves anything out: such a
 // number is on the same side of every border as the float64. (Borders have few bits; what is below
 // 2^-126 of the scale becomes 0.)
-__device__ __forceinline__ uint32_t quantise(const double (&y)[8], uint32_t* scale) {
+__device__ __forceinline__ uint32_t quantise(double (&y)[8], uint32_t* scale) {
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, uint32_t(__double2hiint(y[e])) & 0x7fffffffu);
     const int exponent = group_exponent<20, 1023>(top, scale);
+    if (exponent == 125) {  // a row may be turned beyond what a float32 over 2^e holds
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = fmin(fmax(y[e], -0x1p130), 0x1p130);
+    }
     const int shift = (1023 - 127 + exponent) << 20;
     float m[8];
 #pragma unroll

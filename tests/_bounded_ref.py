@@ -75,7 +75,8 @@ def quantise(x):
     x = torch.where(bad[:, None], 0.0, x)
     top = x.abs().amax(1)
     e = torch.where(top > 0, torch.frexp(top)[1] - 3, -125).clamp(-125, 125)
-    m = x.abs() * torch.exp2(-e.double())[:, None]  # (exact: a power of two)
+    # (exact: a power of two; above 8 a distance's rounding could make 6 as near as 0)
+    m = (x.abs() * torch.exp2(-e.double())[:, None]).clamp(max=8.0)
     order = torch.tensor([0, 2, 4, 6, 1, 3, 5, 7])  # the even codes first
     code = order[(m[..., None] - GRID[order]).abs().argmin(-1)]
     code = code + 8 * torch.signbit(x).long()

@@ -176,6 +176,26 @@ def test_append(gpu, dtype, Hq, H, d, page, new, kv, rot, layout, axes, bad, ord
             assert torch.equal(got[:, :live].cpu().double(), w)
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("factor", [2.0 ** 127, 2.0 ** -140])
+def test_rotations_of_any_factor(gpu, layout, factor):
+    """K beyond what float32 holds: its codes keep their signs, at the largest and smallest scale."""
+    g = torch.Generator().manual_seed(6)
+    K = torch.randn(2, 50, 64, generator=g) * torch.logspace(-30, 37, 50)[:, None]
+    bt = B.Batch4(52, F, 2, 2, 64, 16, (50,), (50,))
+    cache, t, _ = bt.to4("cuda")
+    pos = torch.randint(0, 9000, (1, 50), generator=g, dtype=torch.int32)
+    f = torch.pow(10000.0, -torch.arange(32, dtype=torch.float64) / 32).float()
+    sp.sparsp_paged_append4(K.cuda(), K.cuda(), cache, **t, rotary=sp.Rotary(64, layout, (32,), factor),
+                            positions=pos.cuda(), inv_freq=f.cuda())
+    y, _ = R.rotate(K, pos, f, 64, layout, (32,), factor)
+    got = [x.cpu() for x in cache.tensors]
+    for i in range(50):
+        p, r = bt.place(0, i)
+        codes, scales = B.quantise(y[:, i])
+        assert torch.equal(got[0][p, :, r], codes) and torch.equal(got[1][p, :, :, r], scales), i
+
+
 def test_read_of_a_whole_cache(gpu):
     """new_off as the running sums of kv_len: every cached token, in order."""
     bt = B.Batch4(52, BF, 2, 2, 64, 16, (1, 1, 1), (37, 5, 64))
