@@ -155,9 +155,10 @@ int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sink
  * Row i of the new tables continues the old row parents[i] (outside [0, B): an empty sequence), for
  * any number of rows; old rows that none continues end. Full pages are shared. A page that is filled
  * in part stays with the first row that continues its sequence if its count was 1, and is copied for
- * every other, in all the buffers, to a page of its own (never one that the call copies from). Counts: refs_out is refs less the old
- * table's entries and with the new one's. The old table, counts and lengths stay as they are; contents
- * of pages that it names stay as long as nothing is written to the new one's.
+ * every other, in all the buffers, to a page of its own (never one that the call copies from). Counts:
+ * refs_out is refs less the old table's entries and with the new one's. The old table, counts and
+ * lengths stay as they are; contents of pages that it names stay as long as nothing is written to the
+ * new one's.
  *
  * table_out [rows, width], kv_len_out [rows], refs_out [pages], left [1].
  */

@@ -53,7 +53,6 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(const PagedArgs a, c
     // a page).
     const int list_shift = WINDOW ? 4 : shift;
 
-
     for (int tile = work.tile; tile * int64_t(16 * NC) < rows; tile += work.stride) {
         if constexpr (WINDOW) {
             span = span_of(a, s, G, tile * 16 * NC, min(rows, (tile + 1) * 16 * NC) - 1, KEYS);
@@ -508,8 +507,8 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     r.bytes = parts > 1 ? (parts * part_bytes + unit - 1) / unit * unit : 0;
     // Whole row tiles of 128 in more than one round of two a CU (three at d <= 64), that is 64 an XCD:
     // those of the last round are cut into as many parts as fill it best, for the partial rows of that
-    // round alone (4 bits, 8 key heads, 1,021 and 1,500 tokens over up to 16,384: 85 tiles an XCD, 659
-    // us whole, 558 us with the last 21 in parts).
+    // round alone (4 bits, 8 key heads, 1,021 and 1,500 tokens over up to 16,384: 85 tiles an XCD, 640
+    // us whole, 537 us with the last 21 in parts).
     if ((a.window || a.k_scales) && r.rows == 128 && parts == 1 && !r.plan.flat && pairs % 8 == 0 &&
         tiles == (rows + r.rows - 1) / r.rows) {
         const int64_t slots = (c.d <= 64 ? 3 : 2) * kCus / 8;
