@@ -11,7 +11,8 @@
     sparsp_pages_copy         contents of pages to others
 
 Attention with a window over a cache of rows is sparsp_paged_attn(window=, sinks=). Token tensors, page
-tables, lengths, devices and streams are as for the paged cache (paged.py).
+tables, lengths, devices and streams are as for the paged cache (paged.py). No two tensors of a page
+call of which it writes one may share memory.
 """
 
 from __future__ import annotations

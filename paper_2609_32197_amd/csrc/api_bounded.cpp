@@ -1,5 +1,7 @@
 // C ABI of the bounded cache (sparsp_bounded.h) but for the window over a cache of rows, which is
 // attention like the other (api_cache.cpp): argument checks and dispatch, plain host C++.
+#include <initializer_list>
+
 #include "../../include/sparsp_bounded.h"
 #include "api_checks.h"
 
@@ -139,6 +141,28 @@ int check_workspace(const sparsp_pages* p, int rows, void* workspace, int64_t by
     return SPARSP_OK;
 }
 
+// Device memory of a page call, and whether the call writes it.
+struct Extent {
+    const char* name;
+    const void* at;
+    int64_t bytes;
+    bool written;
+};
+// What a call writes is its alone: kernels index by what they have written (a compaction by its lists
+// in the workspace and by *live, say), so that memory that is two things at once would lead them
+// anywhere.
+int check_extents(std::initializer_list<Extent> all) {
+    for (const Extent* x = all.begin(); x != all.end(); ++x)
+        for (const Extent* y = all.begin(); y != x; ++y) {
+            if (!x->written && !y->written) continue;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x->at), b = reinterpret_cast<uintptr_t>(y->at);
+            if (a < b ? b - a < uintptr_t(x->bytes) : a - b < uintptr_t(y->bytes))
+                return fail(SPARSP_E_INVALID, "%s and %s overlap", y->name, x->name);
+        }
+    return SPARSP_OK;
+}
+int64_t table_bytes(int64_t rows, int width) { return 4 * rows * width; }
+
 sparsp::PageArgs page_args(const sparsp_pages* p) {
     sparsp::PageArgs a = {};
     a.refs = p->refs;
@@ -248,6 +272,14 @@ int sparsp_pages_reserve(const sparsp_pages* pages, const int32_t* new_off, int3
     if (!new_off || !left) return fail(SPARSP_E_INVALID, "new_off or left is NULL");
     sparsp::PageArgs a = page_args(pages);
     if (int rc = check_workspace(pages, pages->B, workspace, workspace_bytes, &a)) return rc;
+    if (int rc = check_extents(
+            {{"refs", pages->refs, 4 * int64_t(pages->pages), true},
+             {"table", pages->table, table_bytes(pages->B, pages->width), true},
+             {"kv_len", pages->kv_len, 4 * int64_t(pages->B), false},
+             {"new_off", new_off, 4 * (int64_t(pages->B) + 1), false},
+             {"left", left, 4, true},
+             {"workspace", workspace, lay_out(pages, pages->B, nullptr, nullptr), true}}))
+        return rc;
     a.moves = nullptr;
     a.from = nullptr;
     a.new_off = new_off;
@@ -260,6 +292,10 @@ int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sink
     if (window < 0 || sinks < 0 || (sinks > 0 && window == 0))
         return fail(SPARSP_E_INVALID, "window = %d and sinks = %d must not be negative, sinks need a window",
                     window, sinks);
+    if (int rc = check_extents({{"refs", pages->refs, 4 * int64_t(pages->pages), true},
+                                {"table", pages->table, table_bytes(pages->B, pages->width), true},
+                                {"kv_len", pages->kv_len, 4 * int64_t(pages->B), false}}))
+        return rc;
     sparsp::PageArgs a = page_args(pages);
     a.window = window < kFarthest ? window : kFarthest;
     a.sinks = sinks;
@@ -282,6 +318,17 @@ int sparsp_pages_fork(const sparsp_pages* pages, const int32_t* parents, int32_t
         return fail(SPARSP_E_INVALID, "a fork's outputs may not be its inputs");
     sparsp::PageArgs a = page_args(pages);
     if (int rc = check_workspace(pages, rows, workspace, workspace_bytes, &a)) return rc;
+    if (int rc = check_extents(
+            {{"refs", pages->refs, 4 * int64_t(pages->pages), false},
+             {"table", pages->table, table_bytes(pages->B, pages->width), false},
+             {"kv_len", pages->kv_len, 4 * int64_t(pages->B), false},
+             {"parents", parents, 4 * int64_t(rows), false},
+             {"table_out", table_out, table_bytes(rows, pages->width), true},
+             {"kv_len_out", kv_len_out, 4 * int64_t(rows), true},
+             {"refs_out", refs_out, 4 * int64_t(pages->pages), true},
+             {"left", left, 4, true},
+             {"workspace", workspace, lay_out(pages, rows, nullptr, nullptr), true}}))
+        return rc;
     a.old_refs = pages->refs;
     a.old_table = pages->table;
     a.refs = refs_out;
@@ -304,6 +351,14 @@ int sparsp_pages_compact(const sparsp_pages* pages, const sparsp_page_buffer* bu
         return fail(SPARSP_E_INVALID, "a compaction's outputs may not be its inputs");
     sparsp::PageArgs a = page_args(pages);
     if (int rc = check_workspace(pages, pages->B, workspace, workspace_bytes, &a)) return rc;
+    if (int rc = check_extents(
+            {{"refs", pages->refs, 4 * int64_t(pages->pages), false},
+             {"table", pages->table, table_bytes(pages->B, pages->width), false},
+             {"table_out", table_out, table_bytes(pages->B, pages->width), true},
+             {"refs_out", refs_out, 4 * int64_t(pages->pages), true},
+             {"live", live, 4, true},
+             {"workspace", workspace, lay_out(pages, pages->B, nullptr, nullptr), true}}))
+        return rc;
     a.old_refs = pages->refs;
     a.old_table = pages->table;
     a.refs = refs_out;
