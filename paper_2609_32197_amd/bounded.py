@@ -285,7 +285,7 @@ def _buffers(caches, pages, dev):
             at, shape = _on(t, "a cache", dev), t.shape
             if len(shape) < 2 or shape[0] != pages:
                 raise ValueError(f"a cache must be [pages = {pages}, ...] (got {tuple(shape)})")
-            packed += _BUFFER.pack(at, t.nbytes // pages)
+            packed += _BUFFER.pack(at, t.nbytes // max(pages, 1))  # (no pages: refused in the call)
             count += 1
     return packed or None, count
 

@@ -51,3 +51,13 @@ def test_arrays_side_by_side(gpu):
     t, r, n, _ = p.compact()
     assert x["table_end"].tolist() == t and x["refs_end"].tolist() == r and int(x["live"]) == n
     assert x["off"].tolist() == [0, 3, 6, 6, 8, 9] and x["parents"].tolist() == parents
+
+
+def test_a_pool_of_no_pages_is_refused(gpu):
+    none, table, kv = ints([]), ints([[0]]), ints([1])
+    x = torch.zeros(0, 8, device="cuda")
+    for call in (lambda: sp.sparsp_pages_fork(none, table, kv, ints([0]), 16, x),
+                 lambda: sp.sparsp_pages_compact(none, table, x),
+                 lambda: sp.sparsp_pages_copy(ints([0]), ints([0]), x)):
+        with pytest.raises(sp.SparspError):
+            call()
