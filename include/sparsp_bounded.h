@@ -160,8 +160,10 @@ int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sink
  * in part stays with the first row that continues its sequence if its count was 1, and is copied for
  * every other, in all the buffers, to a page of its own (never one that the call copies from). Counts:
  * refs_out is refs less the old table's entries and with the new one's. The old table, counts and
- * lengths stay as they are; contents of pages that it names stay as long as nothing is written to the
- * new one's.
+ * lengths stay as they are. So do the contents of pages that the new table names, that are copied from
+ * or that something else holds, as long as nothing is written to the new table's; the pages of old rows
+ * that end are free for the copies, which may overwrite them. A caller who may go back to the old table
+ * counts them once more in refs, and gives that up in refs_out when it is decided.
  *
  * table_out [rows, width], kv_len_out [rows], refs_out [pages], left [1].
  */

@@ -142,7 +142,8 @@ __device__ __forceinline__ uint64_t page_bits(PageBits<N>& lds, int base, Test t
     }
     return bits;
 }
-// Free ones. What a fork copies from is not, though all that held it may have gone.
+// Free ones. What a fork copies from is not, though all that held it may have gone; what only rows that
+// end have held is, so that a fork needs no more pages than the new rows.
 template <int N>
 __device__ __forceinline__ uint64_t free_pages(const PageArgs& a, PageBits<N>& lds, int base) {
     return page_bits<N>(lds, base, [&](int i) {

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2609_32197_amd as sp
-from tests.test_gpu_pages import Pool, ints
+from tests.test_gpu_pages import Pool, ints, moved
 
 pytestmark = pytest.mark.gpu
 I32 = torch.int32
@@ -51,6 +51,60 @@ def test_arrays_side_by_side(gpu):
     t, r, n, _ = p.compact()
     assert x["table_end"].tolist() == t and x["refs_end"].tolist() == r and int(x["live"]) == n
     assert x["off"].tolist() == [0, 3, 6, 6, 8, 9] and x["parents"].tolist() == parents
+
+
+# pages, page, width, kv, parents
+FORKS = [
+    (4, 16, 2, (20, 16), (0, 0)),                       # the copy goes to the page of the row that ends
+    (2, 16, 1, (16, 5), (1, 1)),
+    (40, 16, 5, (1, 16, 17, 0, 80), (2, 2, 0, 0, 2, -1)),
+    (300, 64, 20, (700, 64, 63, 65, 1280, 1), (5, 5, 0, 2, 0, 5, 3, 7)),
+    (3000, 16, 30, tuple(range(1, 400, 3)), tuple(7 * (i // 5) for i in range(90))),
+    (20000, 32, 9, tuple((7 * b) % 289 for b in range(1500)), tuple(3 * (i // 4) for i in range(1600))),
+]
+
+
+@pytest.mark.parametrize("pages,page,width,kv,parents", FORKS)
+@pytest.mark.parametrize("share", [0.0, 0.5])
+@pytest.mark.parametrize("held", [True, False])
+def test_what_the_old_table_names_after_a_fork(gpu, pages, page, width, kv, parents, share, held):
+    """Contents stay on pages that the new table names, that are copied from or that are held; those of
+    rows that end are free for the copies, unless they are counted once more."""
+    p = Pool(12, pages, page, width, kv, share)
+    named = {q for row in p.table for q in row if p.named(q)}
+    ended = {q for b, row in enumerate(p.table) if b not in parents for q in row if p.named(q)}
+    if held:
+        for q in ended:
+            p.refs[q] += 1
+    x = torch.arange(pages, device="cuda")[:, None] * 8 + torch.arange(8, device="cuda")
+    group = (x, (-x).to(I32))
+    before = [t.clone() for t in group]
+    got = sp.sparsp_pages_fork(ints(p.refs), ints(p.table), ints(p.kv), ints(parents), page, group)
+    t, k, r, left, copies = p.fork(parents)
+    assert got[0].tolist() == t and got[1].tolist() == k and got[2].tolist() == r and int(got[3]) == left
+    for a, b in zip(group, moved(before, copies)):
+        assert torch.equal(a, b)
+    copied = {s for s, _ in copies}
+    stay = named if held else {q for q in named if q in copied or any(q in row for row in
+                                                                    p_rows(p, parents))}
+    assert stay
+    for a, b in zip(group, before):
+        i = torch.tensor(sorted(stay), device="cuda")
+        assert torch.equal(a[i], b[i])
+    if held:  # given back, the counts are those of the new table alone
+        for q in ended:
+            r[q] -= 1
+        want = [0] * pages
+        for row in t:
+            for q in row:
+                if q >= 0:
+                    want[q] += 1
+        assert r == want
+
+
+def p_rows(p, parents):
+    """The old rows that go on, without what lies behind their tokens."""
+    return [p.table[b][:-(-p.kv[b] // p.page)] for b in set(parents) if 0 <= b < len(p.table)]
 
 
 def test_a_pool_of_no_pages_is_refused(gpu):
