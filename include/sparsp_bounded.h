@@ -163,7 +163,9 @@ int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sink
  * lengths stay as they are. So do the contents of pages that the new table names, that are copied from
  * or that something else holds, as long as nothing is written to the new table's; the pages of old rows
  * that end are free for the copies, which may overwrite them. A caller who may go back to the old table
- * counts them once more in refs, and gives that up in refs_out when it is decided.
+ * counts them once more in refs, and gives that up in refs_out when it is decided. *left leaves
+ * out pages that were copied from and that nothing holds any longer (a partly filled page that several
+ * rows shared): no copy could go there, but refs_out has them free.
  *
  * table_out [rows, width], kv_len_out [rows], refs_out [pages], left [1].
  */

@@ -354,7 +354,8 @@ def sparsp_pages_fork(refs, page_table, kv_len, parents, page: int, caches=(), p
     Full pages are shared, partly filled ones copied in all `caches` (tensors [pages, ...] or Cache4s)
     for all but the first row that continues a sequence; sequences that none continues end. Returns
     (page_table, kv_len, refs, left); the old tensors stay as they are, but copies may go to pages of
-    sequences that end. To go back to the old table, count those once more in refs beforehand.
+    sequences that end. To go back to the old table, count those once more in refs beforehand. left
+    leaves out pages that were copied from and that nothing holds any longer; they are free now.
     """
     torch = _torch()
     p, dev = _pages(refs, page_table, kv_len, page)

@@ -107,6 +107,26 @@ def p_rows(p, parents):
     return [p.table[b][:-(-p.kv[b] // p.page)] for b in set(parents) if 0 <= b < len(p.table)]
 
 
+@pytest.mark.parametrize("pages,page,width,kv,parents", FORKS)
+def test_left_of_a_fork(gpu, pages, page, width, kv, parents):
+    """The free pages, but for those that were copied from and that nothing holds any longer."""
+    p = Pool(13, pages, page, width, kv)
+    # Every other row with tokens on a partly filled page shares it with the row before.
+    for b in range(1, len(kv), 2):
+        i, j = ((kv[c] - 1) // page for c in (b - 1, b))
+        if kv[b] and kv[b - 1] and kv[b - 1] % page:
+            p.refs[p.table[b][j]] -= 1
+            p.table[b][j] = p.table[b - 1][i]
+            p.refs[p.table[b - 1][i]] += 1
+    for who in (parents, range(len(kv))):
+        got = sp.sparsp_pages_fork(ints(p.refs), ints(p.table), ints(p.kv), ints(list(who)), page)
+        t, _, r, left, copies = p.fork(list(who))
+        assert got[0].tolist() == t and got[2].tolist() == r and int(got[3]) == left
+        let_go = {s for s, _ in copies if r[s] <= 0}
+        if left >= 0:
+            assert int((got[2] <= 0).sum()) == int(got[3]) + len(let_go)
+
+
 def test_a_pool_of_no_pages_is_refused(gpu):
     none, table, kv = ints([]), ints([[0]]), ints([1])
     x = torch.zeros(0, 8, device="cuda")
