@@ -114,10 +114,9 @@ int sparsp_paged_read4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype
  * entries that want them (by row, then by place), so results depend on the arguments only. Where a
  * call runs out of free pages the last of these entries name none, and *left, which otherwise is the
  * number of pages still free, is minus the number that is missing. Whatever these arrays hold, no
- * kernel leaves them, or the buffers. What a call writes, its workspace with it, may overlap no other
- * of its arrays: counts, tables, lengths, offsets, parents and single numbers that do are
- * SPARSP_E_INVALID; that the buffers lie apart from these and from one another is the caller's to see to
- * (the same address twice among them is refused).
+ * kernel leaves them, or the buffers. What a call writes, its workspace and the buffers with it, may
+ * overlap no other memory of its own, or it is SPARSP_E_INVALID. (Not looked at: whether two buffers
+ * overlap that begin at different addresses, and whether a fork's left lies in one.)
  */
 typedef struct {
     int32_t* refs;         /* [pages] */

@@ -141,24 +141,31 @@ int check_workspace(const sparsp_pages* p, int rows, void* workspace, int64_t by
     return SPARSP_OK;
 }
 
-// Device memory of a page call, and whether the call writes it.
+// Device memory of a page call, and whether the call writes it; apart: that it may not lie in a buffer.
 struct Extent {
     const char* name;
     const void* at;
     int64_t bytes;
     bool written;
+    bool apart = true;
 };
+bool overlap(const void* x, int64_t x_bytes, const void* y, int64_t y_bytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    return a < b ? b - a < uintptr_t(x_bytes) : a - b < uintptr_t(y_bytes);
+}
 // What a call writes is its alone: kernels index by what they have written (a compaction by its lists
 // in the workspace and by *live, say), so that memory that is two things at once would lead them
-// anywhere.
-int check_extents(std::initializer_list<Extent> all) {
-    for (const Extent* x = all.begin(); x != all.end(); ++x)
-        for (const Extent* y = all.begin(); y != x; ++y) {
-            if (!x->written && !y->written) continue;
-            const uintptr_t a = reinterpret_cast<uintptr_t>(x->at), b = reinterpret_cast<uintptr_t>(y->at);
-            if (a < b ? b - a < uintptr_t(x->bytes) : a - b < uintptr_t(y->bytes))
+// anywhere. The contents that a call moves are written too.
+int check_extents(std::initializer_list<Extent> all, const sparsp::PageBuffers* f = nullptr,
+                  int64_t pages = 0) {
+    for (const Extent* x = all.begin(); x != all.end(); ++x) {
+        for (const Extent* y = all.begin(); y != x; ++y)
+            if ((x->written || y->written) && overlap(x->at, x->bytes, y->at, y->bytes))
                 return fail(SPARSP_E_INVALID, "%s and %s overlap", y->name, x->name);
-        }
+        for (int i = 0; f && x->apart && i < f->count; ++i)
+            if (overlap(x->at, x->bytes, f->data[i], f->bytes[i] * pages))
+                return fail(SPARSP_E_INVALID, "%s and buffer %d overlap", x->name, i);
+    }
     return SPARSP_OK;
 }
 int64_t table_bytes(int64_t rows, int width) { return 4 * rows * width; }
@@ -326,8 +333,9 @@ int sparsp_pages_fork(const sparsp_pages* pages, const int32_t* parents, int32_t
              {"table_out", table_out, table_bytes(rows, pages->width), true},
              {"kv_len_out", kv_len_out, 4 * int64_t(rows), true},
              {"refs_out", refs_out, 4 * int64_t(pages->pages), true},
-             {"left", left, 4, true},
-             {"workspace", workspace, lay_out(pages, rows, nullptr, nullptr), true}}))
+             {"left", left, 4, true, false},  // (no kernel reads it back)
+             {"workspace", workspace, lay_out(pages, rows, nullptr, nullptr), true}},
+            &f, pages->pages))
         return rc;
     a.old_refs = pages->refs;
     a.old_table = pages->table;
@@ -357,7 +365,8 @@ int sparsp_pages_compact(const sparsp_pages* pages, const sparsp_page_buffer* bu
              {"table_out", table_out, table_bytes(pages->B, pages->width), true},
              {"refs_out", refs_out, 4 * int64_t(pages->pages), true},
              {"live", live, 4, true},
-             {"workspace", workspace, lay_out(pages, pages->B, nullptr, nullptr), true}}))
+             {"workspace", workspace, lay_out(pages, pages->B, nullptr, nullptr), true}},
+            &f, pages->pages))
         return rc;
     a.old_refs = pages->refs;
     a.old_table = pages->table;
@@ -376,6 +385,9 @@ int sparsp_pages_copy(const sparsp_page_buffer* buffers, int32_t count, int32_t 
     if (moves < 0 || moves > (1 << 30)) return fail(SPARSP_E_INVALID, "moves = %d out of range", moves);
     if (moves == 0) return ok();
     if (!src || !dst) return fail(SPARSP_E_INVALID, "src or dst is NULL");
+    if (int rc = check_extents({{"src", src, 4 * int64_t(moves), false}, {"dst", dst, 4 * int64_t(moves), false}},
+                               &f, pages))
+        return rc;
     return hip_status(sparsp::launch_pages_copy(f, src, dst, moves, pages, (hipStream_t)stream),
                       "sparsp_pages_copy");
 }

@@ -1,10 +1,11 @@
-"""The page calls without a GPU: one memory for two of a call's arrays is refused before a launch."""
+"""The page calls without a GPU: one memory for two of a call's arrays, or for an array and the contents
+that it moves, is refused before a launch."""
 
 import pytest
 import torch
 
 import paper_2609_32197_amd as sp
-from paper_2609_32197_amd.bounded import _PAGES
+from paper_2609_32197_amd.bounded import _BUFFER, _PAGES
 
 AT = 1 << 20  # addresses that no refused call touches, this far apart
 PAGES, PAGE, WIDTH, B = 900, 16, 40, 30
@@ -34,8 +35,9 @@ def size(call, name):
     return SIZE[name]
 
 
-def status(call, at):
+def status(call, at, buffers=()):
     """Of the call with these addresses."""
+    packed = b"".join(_BUFFER.pack(*x) for x in buffers) or None
     lib = sp.load_library()
     p = _PAGES.pack(at["refs"], at["table"], at.get("kv_len", 0), PAGES, PAGE, WIDTH, B)
     ws = (at.get("workspace"), size(call, "workspace"), None)
@@ -44,10 +46,10 @@ def status(call, at):
     elif call == "release":
         rc = lib.sparsp_pages_release(p, 5, 2, None)
     elif call == "fork":
-        rc = lib.sparsp_pages_fork(p, at["parents"], ROWS, None, 0, at["table_out"], at["kv_len_out"],
+        rc = lib.sparsp_pages_fork(p, at["parents"], ROWS, packed, len(buffers), at["table_out"], at["kv_len_out"],
                                    at["refs_out"], at["left"], *ws)
     else:
-        rc = lib.sparsp_pages_compact(p, None, 0, at["table_out"], at["refs_out"], at["live"], *ws)
+        rc = lib.sparsp_pages_compact(p, packed, len(buffers), at["table_out"], at["refs_out"], at["live"], *ws)
     return sp.STATUS[rc], lib.sparsp_last_error().decode()
 
 
@@ -70,3 +72,26 @@ def test_overlapping_arrays_are_refused(call, a, b):
             got, message = status(call, at)
             assert got == "SPARSP_E_INVALID", (x, y, off, message)
             assert "overlap" in message or "inputs" in message
+
+
+@pytest.mark.parametrize("call,name", [(c, n) for c in ("fork", "compact") for n in CALLS[c][0]
+                                       if (c, n) != ("fork", "left")])
+def test_arrays_in_the_contents_are_refused(call, name):
+    """At the first and in the last page of the second buffer."""
+    at = {n: (i + 1) * AT for i, n in enumerate(CALLS[call][0])}
+    first, second = 64 * AT, 65 * AT
+    for off in (0, 48 * PAGES - 16):
+        at[name] = second + off
+        got, message = status(call, at, ((first, 16), (second, 48)))
+        assert got == "SPARSP_E_INVALID" and "buffer 1 overlap" in message
+    # The first bytes of the buffer are the array's last.
+    at[name] = second - max(size(call, name) - 16, 0) // 16 * 16
+    got, message = status(call, at, ((first - AT, 16), (second, 48)))
+    assert got == "SPARSP_E_INVALID" and "buffer 1 overlap" in message
+
+
+def test_page_numbers_in_the_contents_are_refused():
+    lib = sp.load_library()
+    for src, dst in ((2 * AT + 64 * PAGES - 16, AT), (AT, 2 * AT)):
+        rc = lib.sparsp_pages_copy(_BUFFER.pack(2 * AT, 64), 1, PAGES, src, dst, 5, None)
+        assert sp.STATUS[rc] == "SPARSP_E_INVALID" and "overlap" in lib.sparsp_last_error().decode()
