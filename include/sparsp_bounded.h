@@ -113,10 +113,12 @@ int sparsp_paged_read4(const sparsp_cache4* cache, int32_t tokens, int32_t dtype
  * host, so a step can be captured. Pages are taken lowest number first, in the order of the
  * entries that want them (by row, then by place), so results depend on the arguments only. Where a
  * call runs out of free pages the last of these entries name none, and *left, which otherwise is the
- * number of pages still free, is minus the number that is missing. Whatever these arrays hold, no
- * kernel leaves them, or the buffers. What a call writes, its workspace and the buffers with it, may
- * overlap no other memory of its own, or it is SPARSP_E_INVALID. (Not looked at: whether two buffers
- * overlap that begin at different addresses, and whether a fork's left lies in one.)
+ * number of pages still free, is minus the number that is missing. Each call sets a *left of its own:
+ * of several in a row (fork, release, reserve) each needs its own memory until all are read, and the
+ * least of them says whether all pages were there. Whatever these arrays hold, no kernel leaves them, or
+ * the buffers. What a call writes, its workspace and the buffers with it, may overlap no other memory of
+ * its own, or it is SPARSP_E_INVALID. (Not looked at: whether two buffers overlap that begin at
+ * different addresses, and whether a fork's left lies in one.)
  */
 typedef struct {
     int32_t* refs;         /* [pages] */
@@ -141,6 +143,9 @@ int64_t sparsp_pages_workspace_bytes(const sparsp_pages* pages, int32_t rows);
  * Pages for the new tokens kv_len - n .. kv_len - 1 of every sequence (n = new_off[b+1] - new_off[b],
  * as for the append that follows): entries among theirs that name no page get a free one, its count
  * 1. The page that a sequence's last old token is on must be its own, as sparsp_pages_fork sees to.
+ * Where that page is missing because an earlier call ran out of pages, the entry names none and gets
+ * one like the others: the old tokens that were to be on it are not, and read as whatever the page
+ * holds. *left does not tell; the earlier call's did (see above).
  */
 int sparsp_pages_reserve(const sparsp_pages* pages, const int32_t* new_off, int32_t* left,
                          void* workspace, int64_t workspace_bytes, void* stream);

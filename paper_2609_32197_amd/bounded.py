@@ -324,7 +324,9 @@ def sparsp_pages_reserve(refs, page_table, new_off, kv_len, page: int, left=None
 
     refs int32 [pages] counts the entries that name a page; it and page_table are changed in place.
     kv_len counts the new tokens. Returns left, int32 [1]: the free pages left, or minus the number
-    that was missing. A workspace is allocated here unless one is given, like left.
+    that was missing. A workspace is allocated here unless one is given, like left. A fork's left is
+    another tensor's: where that was negative, a row's last tokens have no page, and the one that they
+    get here holds anything; torch.minimum of the two tells for both.
     """
     p, dev = _pages(refs, page_table, kv_len, page)
     B = page_table.shape[0]

@@ -127,6 +127,44 @@ def test_left_of_a_fork(gpu, pages, page, width, kv, parents):
             assert int((got[2] <= 0).sum()) == int(got[3]) + len(let_go)
 
 
+def test_a_shortage_is_seen_behind_a_reserve(gpu):
+    """A fork that finds no page for a copy, a release that frees some, a reserve that needs one: each
+    call's left is its own, and the smaller of the two is the turn's, outside a graph and in one."""
+    # One sequence of 70 tokens on pages 0 to 4, the rest held; two rows go on with it.
+    refs, table, kv = ints([1] * 5 + [3] * 3), ints([[0, 1, 2, 3, 4, -1]]), ints([70])
+    parents, off = ints([0, 0]), ints([0, 1, 2])
+    group = torch.arange(8 * 8, device="cuda").view(8, 8)
+    first = group.clone()
+
+    def turn():
+        t, k, r, short = sp.sparsp_pages_fork(refs, table, kv, parents, 16, group)
+        made = t.clone()
+        sp.sparsp_pages_release(r, t, k, 16, window=20)
+        k = k + 1
+        left = sp.sparsp_pages_reserve(r, t, off, k, 16)
+        return made, t, r, short, left, torch.minimum(short, left)
+
+    def check(made, t, r, short, left, both):
+        assert made.tolist() == [[0, 1, 2, 3, 4, -1], [0, 1, 2, 3, -1, -1]] and int(short) == -1
+        # The window's start, pages 0 to 2, is free by now, and the row without a page gets one of
+        # them, on which its six tokens are not.
+        assert t.tolist() == [[-1, -1, -1, 3, 4, -1], [-1, -1, -1, 3, 0, -1]]
+        assert r.tolist() == [1, 0, 0, 2, 1, 3, 3, 3] and int(left) == 2 and int(both) == -1
+        assert torch.equal(group, first)
+
+    check(*turn())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = turn()
+    for _ in range(3):
+        for x in got:
+            x.fill_(-77)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(*got)
+        check(*turn())
+
+
 def test_a_pool_of_no_pages_is_refused(gpu):
     none, table, kv = ints([]), ints([[0]]), ints([1])
     x = torch.zeros(0, 8, device="cuda")
