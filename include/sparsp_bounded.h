@@ -171,6 +171,10 @@ int sparsp_pages_release(const sparsp_pages* pages, int32_t window, int32_t sink
  * out pages that were copied from and that nothing holds any longer (a partly filled page that several
  * rows shared): no copy could go there, but refs_out has them free.
  *
+ * Rows that share pages can be attended, appended to and forked on, and sparsp_pages_compact keeps them
+ * shared. sparsp_paged_weights and sparsp_cache_evict take no shared pages: two rows would write the
+ * same weights, and an eviction of one moves the other's tokens. A cache is cut before it is forked.
+ *
  * table_out [rows, width], kv_len_out [rows], refs_out [pages], left [1].
  */
 int sparsp_pages_fork(const sparsp_pages* pages, const int32_t* parents, int32_t rows,

@@ -358,6 +358,7 @@ def sparsp_pages_fork(refs, page_table, kv_len, parents, page: int, caches=(), p
     (page_table, kv_len, refs, left); the old tensors stay as they are, but copies may go to pages of
     sequences that end. To go back to the old table, count those once more in refs beforehand. left
     leaves out pages that were copied from and that nothing holds any longer; they are free now.
+    Rows that share pages are not for sparsp_paged_weights or sparsp_cache_evict.
     """
     torch = _torch()
     p, dev = _pages(refs, page_table, kv_len, page)

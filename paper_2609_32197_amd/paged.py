@@ -394,7 +394,8 @@ def sparsp_paged_weights(Q, lse, K_cache, page_table, new_off, kv_len, weights,
     """Adds (or with accumulate=False writes) the attention weight of every cached token.
 
     Q, lse and the other arguments as given to and returned by sparsp_paged_attn; weights
-    float32 [pages, H, page]. Returns weights.
+    float32 [pages, H, page]. Returns weights. No two sequences may share a page (as they do after
+    sparsp_pages_fork).
     """
     torch = _torch()
     c, dev = _cache(K_cache, None, weights, page_table, new_off, kv_len)
@@ -421,7 +422,8 @@ def sparsp_cache_evict(K_cache, V_cache, weights, page_table, kv_len, keep: int,
     The kept tokens move to the front of the sequence's pages, or into the pages of dst_table
     (int32 [B, width], none of them in page_table). kept lists them, ascending, then -1. Few long
     sequences use a workspace (sparsp_cache_evict_workspace_bytes bytes), which is allocated here
-    unless one is given, like the outputs.
+    unless one is given, like the outputs. No two sequences may share a page (as they do after
+    sparsp_pages_fork): cutting one would move the other's tokens.
     """
     torch = _torch()
     c, dev = _cache(K_cache, V_cache, weights, page_table, None, kv_len)
