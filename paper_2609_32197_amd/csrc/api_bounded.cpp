@@ -385,7 +385,8 @@ int sparsp_pages_copy(const sparsp_page_buffer* buffers, int32_t count, int32_t 
     if (moves < 0 || moves > (1 << 30)) return fail(SPARSP_E_INVALID, "moves = %d out of range", moves);
     if (moves == 0) return ok();
     if (!src || !dst) return fail(SPARSP_E_INVALID, "src or dst is NULL");
-    if (int rc = check_extents({{"src", src, 4 * int64_t(moves), false}, {"dst", dst, 4 * int64_t(moves), false}},
+    if (int rc = check_extents({{"src", src, 4 * int64_t(moves), false},
+                                {"dst", dst, 4 * int64_t(moves), false}},
                                &f, pages))
         return rc;
     return hip_status(sparsp::launch_pages_copy(f, src, dst, moves, pages, (hipStream_t)stream),

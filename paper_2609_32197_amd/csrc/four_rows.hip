@@ -12,10 +12,18 @@
 //
 // A thread takes eight channels, a dword of codes; four neighbours share a scale. A workgroup takes
 // `per` tokens and shares their cosines and sines over all heads, as in rotate_rows.hip. Prompts of
-// 8,400 tokens, 20 heads of Q, K and V of 128, half of each rotated: 56 us, 3.4 TB/s, the vector unit
-// busy with the 64-bit rotation (with codes by comparisons in 64 bits instead of the conversion
-// instruction 77 us); the same read back 25 us, 4.4 TB/s. With 2 or 4
-// tokens a workgroup both take 79 us, with one 88, with eight 85.
+// 8,461 tokens, 20 heads of Q, K and V of 128, half of each rotated: 56 us, 3.4 TB/s, the vector unit
+// busy with the 64-bit rotation, which K's channels behind the rotated ones go through too, turned by
+// nothing (with codes by comparisons in 64 bits instead of the conversion instruction 77 us); the same
+// read back 25 us, 4.4 TB/s.
+//
+// `per` is chosen by the tokens alone, whatever the heads; many heads would have shorter runs and few
+// longer ones. Append and read, us, the same data over and over, at most 4, 8 and 16 tokens:
+//   20 heads of Q, K and V, 8,461 tokens    45 + 23    49 + 24    49 + 24 (the rule takes 8)
+//   20 heads,              50,895 tokens   258 + 159  271 + 164  287 + 169
+//   32 and 8 heads,       111,075 tokens   450 + 130  474 + 136  500 + 141
+//   8 and 2 heads of 64,  111,075 tokens   126 + 34   104 + 30    94 + 26
+//   one head,             111,075 tokens    96 + 34    78 + 30    69 + 26
 #include "cache_device.h"
 #include "paged_four.h"
 
@@ -327,7 +335,8 @@ Params params(const FourArgs& f, int pairs) {
     p.cache = a.cache;
     p.units = make_div(uint32_t(a.cache.d / 8));
     p.heads = make_div(uint32_t(a.cache.H));
-    // As in rotate_rows.hip: enough workgroups to fill the GPU four times, then longer runs.
+    // As in rotate_rows.hip: enough workgroups to fill the GPU four times, then longer runs (figures
+    // at the top).
     int per = 1;
     while (per < kMaxPer && a.tokens / (2 * per) >= 1024 &&
            (pairs == 0 || 2 * per * (pairs + kStill) <= kTablePairs))

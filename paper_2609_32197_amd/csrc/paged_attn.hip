@@ -483,7 +483,9 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
         parts = rounds <= 8 ? 1 : std::min(parts, (rounds + 3) / 4);
         // Where a window bounds the longest sequences, those that reach it are many and end together
         // (64 sequences of 400 to 32,768, one new token each: window 2,048 85 us whole, 98 us in 2
-        // parts; 4,096 142 and 154; 8,192 239 whole, 224 in 5).
+        // parts; 4,096 142 and 154; 8,192 239 whole, 224 in 5). Whether the window does bound them is
+        // not asked: of 64 sequences of 400 to 5,000 a window of 8,192 takes 130 us whole, where
+        // without a window they take 110 us in 3 parts (over 4 bits 41 and 38).
         if (a.window && !tall && fill == 1 && rounds * round <= 5120) parts = 1;
     }
     const int64_t all_rows = int64_t(a.q_heads) * a.tokens, part_bytes = all_rows * (c.d + 2) * 4;
@@ -507,8 +509,12 @@ Shape shape(const PagedArgs& a, int64_t ws_bytes) {
     r.bytes = parts > 1 ? (parts * part_bytes + unit - 1) / unit * unit : 0;
     // Whole row tiles of 128 in more than one round of two a CU (three at d <= 64), that is 64 an XCD:
     // those of the last round are cut into as many parts as fill it best, for the partial rows of that
-    // round alone (4 bits, 8 key heads, 1,021 and 1,500 tokens over up to 16,384: 85 tiles an XCD, 640
-    // us whole, 537 us with the last 21 in parts).
+    // round alone (4 bits, 8 key heads, 1,066 and 1,500 tokens over up to 16,384: 81 tiles an XCD, 642
+    // us whole, 539 us with the last 17 in three parts, 48 MB). The share of a round that a part is
+    // counted as costing does not know how long a round is: of 2,048 and 1,531 tokens the last 48 of
+    // 112 tiles are cut in four, 136 MB, which long walks gain by (4 bits, over 32,768 keys 1,419 and
+    // 1,522 us whole) and short ones lose by (window 4,096, bf16 328 and 254 us, 4 bits 361 and 282;
+    // 16,384, bf16 929 and 893). A workspace too small for the parts leaves the tiles whole.
     if ((a.window || a.k_scales) && r.rows == 128 && parts == 1 && !r.plan.flat && pairs % 8 == 0 &&
         tiles == (rows + r.rows - 1) / r.rows) {
         const int64_t slots = (c.d <= 64 ? 3 : 2) * kCus / 8;

@@ -4,13 +4,15 @@
 // of the keys a workgroup, four waves that walk tiles of 32 keys in turn with a softmax each, the next
 // tile loading while one is computed, joined in LDS. A tile is a quarter of the bytes of bf16, and
 // making bf16 of it costs vector instructions (32 conversions and 32 permutations a lane for a tile of
-// d = 128), so what bounds it is their issue as much as reading: everything else in the loop is kept
-// from the vector unit. A tile's page is the same for all lanes, so its address is scalar, and lanes
-// add constants. The reference of a row's exponentials moves only where they grow past it, as in
-// paged_attn_tiles.hip, so a tile takes no maximum and rescales nothing. 64 sequences of 400 to 9,001
-// tokens, 8 key heads, one new token each: 46 us (184 MB, 4.0 TB/s; of 9,000 each 5.0 TB/s, 192 of
-// them 5.65), 59 us as one more tile type of paged_rows_kernel. One tile in flight and four waves a
-// SIMD spill (64 of 9,000: 172 us), two waves and three tiles gain nothing (126.8 and 126.8 us).
+// d = 128), so everything else in the loop is kept from the vector unit. A tile's page is the same for
+// all lanes, so its address is scalar, and lanes add constants. The reference of a row's exponentials
+// moves only where they grow past it, as in paged_attn_tiles.hip, so a tile takes no maximum and
+// rescales nothing. 64 sequences of 400 to 9,001 tokens, 8 key heads, one new token each: 46 us (184
+// MB, 4.0 TB/s), 59 us as one more tile type of paged_rows_kernel. Neither issue (38% of it) nor reading
+// is full then: parts of 1,920 keys make 968 workgroups of 1 to 15 rounds of 128 keys for the 768 that
+// the registers and LDS let reside. Sequences of 9,000 each: 4.9 TB/s in 5 parts, 5.4 whole, 192 of them
+// 5.4 and 5.7. One tile in flight and four waves a SIMD spill (64 of 9,000: 172 us), two waves and three
+// tiles gain nothing (126.8 and 126.8 us).
 #include "paged_four.h"
 
 namespace sparsp {

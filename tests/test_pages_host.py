@@ -46,10 +46,11 @@ def status(call, at, buffers=()):
     elif call == "release":
         rc = lib.sparsp_pages_release(p, 5, 2, None)
     elif call == "fork":
-        rc = lib.sparsp_pages_fork(p, at["parents"], ROWS, packed, len(buffers), at["table_out"], at["kv_len_out"],
-                                   at["refs_out"], at["left"], *ws)
+        rc = lib.sparsp_pages_fork(p, at["parents"], ROWS, packed, len(buffers), at["table_out"],
+                                   at["kv_len_out"], at["refs_out"], at["left"], *ws)
     else:
-        rc = lib.sparsp_pages_compact(p, packed, len(buffers), at["table_out"], at["refs_out"], at["live"], *ws)
+        rc = lib.sparsp_pages_compact(p, packed, len(buffers), at["table_out"], at["refs_out"],
+                                      at["live"], *ws)
     return sp.STATUS[rc], lib.sparsp_last_error().decode()
 
 
